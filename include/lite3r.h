@@ -268,6 +268,111 @@ LITE3R_API lite3r_status lite3r_qkv_project_fp8(const unsigned char* x_codes, co
                                      lite3r_fp8 q_out, lite3r_fp8 k_out, lite3r_fp8 v_out, int* device_status,
                                      void* stream);
 
+/* ---- Between the projection and the attention: norms of queries and keys for each head and the rotation by the tokens'
+ * positions, as the transformer blocks that the method is applied to have them (VGGT: layer norm over the 64 values of a head,
+ * then rotary embeddings of the patch's row and column, base 100). ---- */
+typedef enum { LITE3R_NORM_NONE = 0, LITE3R_NORM_RMS = 1, LITE3R_NORM_LAYER = 2 } lite3r_norm;
+
+/* What happens to every row x of head_dim values of a (batch, head, token):
+ *   LAYER: xh = (x - mean) / sqrt(var + eps) (biased variance);  RMS: xh = x / sqrt(mean(x^2) + eps);  NONE: xh = x;
+ *   z = xh * weight + bias;
+ *   rotation: z is cut into `axes` sections of S = head_dim / axes values, section a turns with coordinate a of the token's
+ *   position: the pair (z[i], z[i + S/2]), i < S/2, by the angle position * base^(-2 i / S):
+ *     y[i] = z[i] cos - z[i + S/2] sin,   y[i + S/2] = z[i + S/2] cos + z[i] sin.
+ * In fp32 (angles in fp64, so that positions of any size keep their angle), rounded once. */
+typedef struct {
+  int batch, q_heads, k_heads, tokens, head_dim; /* head_dim 32, 64, 128 or 256; k_heads need not equal q_heads; 0: no keys */
+  lite3r_norm norm;
+  float eps;
+  const float *q_weight, *q_bias, *k_weight, *k_bias; /* DEVICE fp32 [head_dim], 16-byte aligned, or NULL: 1 and 0 */
+  int axes;                                            /* 0: no rotation; 1: along the sequence; 2: row and column */
+  const int* positions; /* DEVICE int32 [batch][tokens][axes] (not read when axes is 0), of any sign; strides in elements, */
+  long long position_stride_b, position_stride_n; /* stride 0 for positions that sequences (or tokens) share */
+  double base;                                    /* > 0 */
+} lite3r_rope;
+
+/* Queries and keys of one attention call in one launch.  q, k: DEVICE [batch, heads, tokens, head_dim] in fp32, bf16 or fp16 with
+ * any batch / head / token strides (multiples of 8 elements, 0 for broadcast dimensions) and contiguous head_dim; all of one
+ * dtype, 16-byte aligned.  q_out, k_out: the results (`ptr` is written), of the same dtype; their rows must not overlap one
+ * another; a result may take the place of its own source (same pointer and strides), otherwise it must not overlap any source.
+ * k and k_out are NULL when k_heads is 0.  Single tokens (decoding) are calls with tokens = 1 and their positions. */
+LITE3R_API lite3r_status lite3r_qk_norm_rope(const lite3r_tensor* q, const lite3r_tensor* k, const lite3r_rope* how,
+                                  const lite3r_tensor* q_out, const lite3r_tensor* k_out, void* stream);
+
+/* Bytes of scratch of lite3r_qk_norm_rope_backward.  Host-only. */
+LITE3R_API lite3r_status lite3r_qk_norm_rope_workspace(int head_dim, size_t* bytes);
+
+/* Gradients with respect to the weights and biases: DEVICE fp32 [head_dim], each may be NULL. */
+typedef struct {
+  float *q_weight, *q_bias, *k_weight, *k_bias;
+} lite3r_rope_grads;
+
+/* Gradient of lite3r_qk_norm_rope.  With g the gradient turned back by the rotation and gh = g * weight:
+ *   d_weight = sum of g * xh,  d_bias = sum of g  over batch, heads and tokens;
+ *   dx = (gh - mean(gh) - xh mean(gh xh)) / sqrt(var + eps)   (RMS: without mean(gh);  NONE: dx = gh).
+ * q, k: the sources of the forward (before the norm); dq_out, dk_out: the gradients of its results; dq, dk: written, one row
+ * for every row of q and k also where the sources are broadcast.  All tensors as in the forward; dq may take the place of q or
+ * of dq_out, dk that of k or dk_out.  Sums are fp32 in a fixed order.  workspace: DEVICE, 256-byte aligned,
+ * lite3r_qk_norm_rope_workspace() bytes. */
+LITE3R_API lite3r_status lite3r_qk_norm_rope_backward(const lite3r_tensor* q, const lite3r_tensor* k, const lite3r_tensor* dq_out,
+                                           const lite3r_tensor* dk_out, const lite3r_rope* how, const lite3r_tensor* dq,
+                                           const lite3r_tensor* dk, const lite3r_rope_grads* grads, void* workspace,
+                                           size_t workspace_bytes, void* stream);
+
+/* ---- Microscaled formats: the 4-bit form of the linear layers, and activations kept in 8 bits for the backward pass. ---- */
+
+/* Blocks of 32 values along a row share a scale 2^E, kept as the byte E + 127 (0xFF: NaN); elements are e2m1 (MXFP4, values up
+ * to 6) or e4m3 (MXFP8, values up to 448). */
+typedef enum { LITE3R_MXFP4 = 0, LITE3R_MXFP8 = 1 } lite3r_mx_format;
+
+/* Bytes of the two buffers of a microscaled matrix [rows, cols] (cols a multiple of 32):
+ *   codes   MXFP8: [rows][cols];  MXFP4: [rows][cols / 2], the element of the even column in the low half of the byte
+ *   scales  [ceil(rows / 128)][ceil(cols / 128)][32][4][4]: the byte of row r, block j (columns 32 j ...) lies at
+ *           [r / 128][j / 4][r % 32][(r % 128) / 32][j % 4], the layout in which the tensor cores take them.
+ * Host-only. */
+LITE3R_API lite3r_status lite3r_mx_sizes(lite3r_mx_format format, int rows, int cols, size_t* codes_bytes, size_t* scales_bytes);
+
+/* Quantiser: E = the smallest integer, at least -127, with max |x| of the block <= top * 2^E (top = 6 or 448), so nothing
+ * saturates; code = round to nearest even (x / 2^E).  A block that holds an infinity or a NaN stands for NaN throughout.
+ * x: DEVICE, fp32, bf16 or fp16, 16-byte aligned, row_stride in elements (a multiple of 8, >= cols).
+ * codes, scales: DEVICE, 16-byte aligned; places of the scales past the matrix are set to zero. */
+LITE3R_API lite3r_status lite3r_quantize_mx(const void* x, lite3r_dtype dtype, long long row_stride, int rows, int cols,
+                                 lite3r_mx_format format, unsigned char* codes, unsigned char* scales, void* stream);
+
+/* The values that a microscaled matrix stands for, rounded once to out's dtype (exact in fp32 and, but for values below its
+ * smallest normal one, in bf16).  out: DEVICE [rows, cols] as x above. */
+LITE3R_API lite3r_status lite3r_dequantize_mx(const unsigned char* codes, const unsigned char* scales, lite3r_mx_format format,
+                                   int rows, int cols, void* out, lite3r_dtype dtype, long long row_stride, void* stream);
+
+/* y = Q(x) Q(W)^T + b on MXFP4 operands with block-scaled products and fp32 accumulation on the tensor cores.
+ * x_codes, x_scales: [rows, d_in]; w_codes, w_scales: [d_out, d_in] (the layout of an nn.Linear weight), as lite3r_quantize_mx
+ * writes them; d_in a multiple of 32 (else LITE3R_ERR_UNSUPPORTED).  bias: DEVICE fp32 [d_out] or NULL.
+ * y: DEVICE [rows, d_out] of y_dtype, row pitch y_stride elements (a multiple of 8), 16-byte aligned.
+ * device_status as for lite3r_sla_forward (cleared by the call). */
+LITE3R_API lite3r_status lite3r_linear_mxfp4(const unsigned char* x_codes, const unsigned char* x_scales, const unsigned char* w_codes,
+                                  const unsigned char* w_scales, const float* bias, int rows, int d_in, int d_out, void* y,
+                                  lite3r_dtype y_dtype, long long y_stride, int* device_status, void* stream);
+
+/* Bytes of scratch of lite3r_linear_mx_wgrad.  Host-only. */
+LITE3R_API lite3r_status lite3r_linear_mx_workspace(int rows, int d_in, int d_out, size_t* bytes);
+
+/* Gradient of a linear layer's input through its quantised weight (the quantisers pass gradients straight through):
+ * dx = dy . Q(W), bf16 x codes (which become bf16 exactly) with fp32 accumulation.  dy: DEVICE bf16 [rows, d_out], row pitch
+ * dy_stride elements (a multiple of 8), 16-byte aligned; w_codes, w_scales: [d_out, d_in] in `format`; dx: DEVICE [rows, d_in]
+ * of dx_dtype, row pitch dx_stride elements (a multiple of 8), 16-byte aligned. */
+LITE3R_API lite3r_status lite3r_linear_mx_dgrad(const void* dy, long long dy_stride, const unsigned char* w_codes,
+                                     const unsigned char* w_scales, lite3r_mx_format format, int rows, int d_in, int d_out,
+                                     void* dx, lite3r_dtype dx_dtype, long long dx_stride, int* device_status, void* stream);
+
+/* Gradient of a linear layer's weight and bias from the kept form of its input: dw = dy^T . C(x), db = sum of dy over the rows.
+ * dy as above; x_codes, x_scales: [rows, d_in] in `format` (MXFP8 for activations that were kept for this); dw: DEVICE fp32
+ * [d_out, d_in], 16-byte aligned; db: DEVICE fp32 [d_out] or NULL.  Partial sums over the rows are added in a fixed order.
+ * workspace: DEVICE, 256-byte aligned, lite3r_linear_mx_workspace() bytes. */
+LITE3R_API lite3r_status lite3r_linear_mx_wgrad(const void* dy, long long dy_stride, const unsigned char* x_codes,
+                                     const unsigned char* x_scales, lite3r_mx_format format, int rows, int d_in, int d_out,
+                                     float* dw, float* db, void* workspace, size_t workspace_bytes, int* device_status,
+                                     void* stream);
+
 /* ---- Training side of the linear-branch projection, the only tensor the method trains (Sec. 3.3 "selective
  * freezing": gradients are applied only to the linear-branch projection layers; Sec. 3.5 Eq. 3). ---- */
 

@@ -20,6 +20,8 @@ SOURCE_DTYPES = {torch.float32: F32, torch.bfloat16: BF16}
 OUT_DTYPES = {torch.float32: F32, torch.bfloat16: BF16, torch.float16: F16}
 PHI_SOFTMAX, PHI_ELU1 = 0, 1
 PHI_CODES = {"softmax": PHI_SOFTMAX, "elu1": PHI_ELU1}
+NORM_CODES = {"none": 0, "rms": 1, "layer": 2}
+MX_FORMATS = {"mxfp4": 0, "mxfp8": 1}
 
 
 class Lite3rError(RuntimeError):
@@ -52,6 +54,17 @@ class Step(C.Structure):
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("device_status", C.c_void_p)]
 
 
+class Rope(C.Structure):
+    _fields_ = [("batch", C.c_int), ("q_heads", C.c_int), ("k_heads", C.c_int), ("tokens", C.c_int), ("head_dim", C.c_int),
+                ("norm", C.c_int), ("eps", C.c_float), ("q_weight", C.c_void_p), ("q_bias", C.c_void_p),
+                ("k_weight", C.c_void_p), ("k_bias", C.c_void_p), ("axes", C.c_int), ("positions", C.c_void_p),
+                ("position_stride_b", C.c_longlong), ("position_stride_n", C.c_longlong), ("base", C.c_double)]
+
+
+class RopeGrads(C.Structure):
+    _fields_ = [("q_weight", C.c_void_p), ("q_bias", C.c_void_p), ("k_weight", C.c_void_p), ("k_bias", C.c_void_p)]
+
+
 EXPORTS = ("lite3r_fp8_sizes", "lite3r_plan_sizes", "lite3r_forward_workspace", "lite3r_quantize_fp8",
            "lite3r_sla_plan", "lite3r_sla_forward", "lite3r_status_string", "lite3r_last_cuda_error",
            "lite3r_launch_count", "lite3r_profile_enable", "lite3r_profile_stage_ms",
@@ -59,7 +72,10 @@ EXPORTS = ("lite3r_fp8_sizes", "lite3r_plan_sizes", "lite3r_forward_workspace", 
            "lite3r_sla_forward_begin", "lite3r_sla_forward_finish", "lite3r_forward_workspace_planned",
            "lite3r_workspace_layout", "lite3r_quantize_rows_fp8", "lite3r_linear_fp8", "lite3r_qkv_project_fp8",
            "lite3r_train_workspace", "lite3r_sla_linear_branch", "lite3r_mse_distill", "lite3r_proj_lin_backward",
-           "lite3r_plan_variant", "lite3r_attention_plain_stores", "lite3r_sla_step")
+           "lite3r_plan_variant", "lite3r_attention_plain_stores", "lite3r_sla_step",
+           "lite3r_qk_norm_rope", "lite3r_qk_norm_rope_workspace", "lite3r_qk_norm_rope_backward", "lite3r_mx_sizes",
+           "lite3r_quantize_mx", "lite3r_dequantize_mx", "lite3r_linear_mxfp4", "lite3r_linear_mx_workspace",
+           "lite3r_linear_mx_dgrad", "lite3r_linear_mx_wgrad")
 STATIC_SCRATCH_BYTES = 32 << 20  # LITE3R_STATIC_SCRATCH_BYTES
 
 
@@ -126,6 +142,20 @@ def lib() -> C.CDLL:
     L.lite3r_proj_lin_backward.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(Shape), C.c_void_p, C.c_void_p, C.c_size_t,
                                            C.c_void_p, C.c_void_p]
     L.lite3r_proj_lin_backward.restype = C.c_int
+    tp, vp, ll = C.POINTER(Tensor), C.c_void_p, C.c_longlong
+    for name, argtypes in {
+            "lite3r_qk_norm_rope": [tp, tp, C.POINTER(Rope), tp, tp, vp],
+            "lite3r_qk_norm_rope_workspace": [C.c_int, sz],
+            "lite3r_qk_norm_rope_backward": [tp, tp, tp, tp, C.POINTER(Rope), tp, tp, C.POINTER(RopeGrads), vp, C.c_size_t, vp],
+            "lite3r_mx_sizes": [C.c_int, C.c_int, C.c_int, sz, sz],
+            "lite3r_quantize_mx": [vp, C.c_int, ll, C.c_int, C.c_int, C.c_int, vp, vp, vp],
+            "lite3r_dequantize_mx": [vp, vp, C.c_int, C.c_int, C.c_int, vp, C.c_int, ll, vp],
+            "lite3r_linear_mxfp4": [vp, vp, vp, vp, vp, C.c_int, C.c_int, C.c_int, vp, C.c_int, ll, vp, vp],
+            "lite3r_linear_mx_workspace": [C.c_int, C.c_int, C.c_int, sz],
+            "lite3r_linear_mx_dgrad": [vp, ll, vp, vp, C.c_int, C.c_int, C.c_int, C.c_int, vp, C.c_int, ll, vp, vp],
+            "lite3r_linear_mx_wgrad": [vp, ll, vp, vp, C.c_int, C.c_int, C.c_int, C.c_int, vp, vp, vp, C.c_size_t, vp, vp]}.items():
+        getattr(L, name).argtypes = argtypes
+        getattr(L, name).restype = C.c_int
     L.lite3r_selftest_wait_expiry.argtypes = [C.c_void_p, C.c_ulonglong, C.c_void_p]
     L.lite3r_selftest_wait_expiry.restype = C.c_int
     L.lite3r_status_string.argtypes = [C.c_int]
@@ -432,6 +462,228 @@ def lite3r_qkv_project_fp8(x_codes, x_scales, w_codes, w_scales, bias, shape: Sh
                                         x_codes.shape[1], q_out.c_struct(), k_out.c_struct(), v_out.c_struct(),
                                         device_status.data_ptr() if device_status is not None else None,
                                         _stream_ptr(stream)), "lite3r_qkv_project_fp8")
+
+
+# ----------------------------------------------------------------------------- norms and rotation of queries and keys
+def _on_current_device(what: str, *tensors) -> None:
+    """Kernels run on the current device: every tensor (None: not given) has to be there."""
+    current = torch.cuda.current_device() if torch.cuda.is_initialized() else None
+    for x in tensors:
+        if x is not None and (not x.is_cuda or x.device.index != current):
+            raise Lite3rError(f"{what}: tensors must be on the current CUDA device")
+
+
+def _bytes_of(workspace, what: str) -> int:
+    """Bytes of a scratch tensor; its pointer alone says where it is, so it has to be contiguous."""
+    if workspace is None or not workspace.is_contiguous():
+        raise Lite3rError(f"{what}: workspace must be a contiguous CUDA tensor")
+    return workspace.numel() * workspace.element_size()
+
+
+def _rows_of_heads(x, like, what: str) -> Tensor:
+    if x.dim() != 4 or x.stride(3) != 1 or x.dtype not in OUT_DTYPES:
+        raise Lite3rError(f"{what}: q, k and their results must be float32 / bfloat16 / float16 [B,H,N,D] with contiguous D")
+    if x.dtype != like.dtype or x.shape[0] != like.shape[0] or x.shape[2:] != like.shape[2:]:
+        raise Lite3rError(f"{what}: one dtype, batch, number of tokens and head dimension for all tensors")
+    return Tensor(x.data_ptr(), OUT_DTYPES[x.dtype], x.stride(0), x.stride(1), x.stride(2))
+
+
+def _vector(x, dim: int, what: str):
+    if x is None:
+        return None
+    if x.dtype != torch.float32 or x.dim() != 1 or x.shape[0] != dim or not x.is_contiguous():
+        raise Lite3rError(f"{what}: weights, biases and their gradients must be contiguous float32 [head_dim]")
+    return x.data_ptr()
+
+
+def _rope(q, k, norm, q_weight, q_bias, k_weight, k_bias, eps, positions, base, what: str) -> Rope:
+    if norm not in NORM_CODES:
+        raise Lite3rError(f"{what}: norm must be one of {', '.join(NORM_CODES)}")
+    batch, heads, tokens, dim = q.shape
+    affine = [_vector(x, dim, what) for x in (q_weight, q_bias, k_weight, k_bias)]
+    axes = stride_b = stride_n = 0
+    if positions is not None:
+        p = positions if positions.dim() == 3 else positions[None]  # [N, axes]: shared by the sequences
+        if p.dtype != torch.int32 or p.dim() != 3 or p.shape[0] not in (1, batch) or p.shape[1] != tokens or p.shape[2] not in (1, 2):
+            raise Lite3rError(f"{what}: positions must be int32 [B, N, axes] or [N, axes] with one or two axes")
+        axes = p.shape[2]
+        if axes == 2 and p.stride(2) != 1:
+            raise Lite3rError(f"{what}: a position's two coordinates must lie next to each other")
+        stride_b, stride_n = p.stride(0) if p.shape[0] > 1 else 0, p.stride(1)
+    return Rope(batch, heads, k.shape[1] if k is not None else 0, tokens, dim, NORM_CODES[norm], eps, *affine, axes,
+                positions.data_ptr() if positions is not None else None, stride_b, stride_n, base)
+
+
+def lite3r_qk_norm_rope(q: torch.Tensor, k, q_out: torch.Tensor, k_out, norm: str = "layer", q_weight=None, q_bias=None,
+                        k_weight=None, k_bias=None, eps: float = 1e-5, positions=None, base: float = 100.0, stream=None) -> None:
+    """Norm of every head's queries and keys and the rotation by the tokens' positions, in one launch.
+
+    q, k: CUDA [B,H,N,D] (views of a packed projection, say; k may have another number of heads, or be None), D 32, 64,
+    128 or 256, fp32 / bf16 / fp16.  q_out, k_out: results of the same dtype, which may be q and k themselves.
+    norm: "layer", "rms" or "none"; weights and biases fp32 [D] or None.  positions: int32 [B,N,axes] or [N,axes]: two axes
+    (row and column) for images, one for sequences; None: no rotation."""
+    what = "lite3r_qk_norm_rope"
+    _on_current_device(what, q, k, q_out, k_out, q_weight, q_bias, k_weight, k_bias, positions)
+    if (k is None) != (k_out is None):
+        raise Lite3rError(f"{what}: k and k_out go together")
+    tensors = [_rows_of_heads(x, q, what) if x is not None else None for x in (q, k, q_out, k_out)]
+    if q_out.shape != q.shape or (k is not None and k_out.shape != k.shape):
+        raise Lite3rError(f"{what}: results must have their sources' shapes")
+    how = _rope(q, k, norm, q_weight, q_bias, k_weight, k_bias, eps, positions, base, what)
+    _check(lib().lite3r_qk_norm_rope(tensors[0], tensors[1], how, tensors[2], tensors[3], _stream_ptr(stream)), what)
+
+
+def lite3r_qk_norm_rope_workspace(head_dim: int) -> int:
+    a = C.c_size_t()
+    _check(lib().lite3r_qk_norm_rope_workspace(head_dim, C.byref(a)), "lite3r_qk_norm_rope_workspace")
+    return a.value
+
+
+def lite3r_qk_norm_rope_backward(q: torch.Tensor, k, dq_out: torch.Tensor, dk_out, dq: torch.Tensor, dk, workspace: torch.Tensor,
+                                 norm: str = "layer", q_weight=None, k_weight=None, dq_weight=None, dq_bias=None,
+                                 dk_weight=None, dk_bias=None, eps: float = 1e-5, positions=None, base: float = 100.0,
+                                 stream=None) -> None:
+    """Gradient of lite3r_qk_norm_rope: dq, dk (written; dq may be q or dq_out, dk likewise) and, where given, the
+    gradients of the weights and biases (fp32 [D]).  q, k: the forward's sources; dq_out, dk_out: gradients of its
+    results.  workspace: lite3r_qk_norm_rope_workspace(D) bytes."""
+    what = "lite3r_qk_norm_rope_backward"
+    _on_current_device(what, q, k, dq_out, dk_out, dq, dk, workspace, q_weight, k_weight, dq_weight, dq_bias, dk_weight,
+                       dk_bias, positions)
+    if not (k is None) == (dk_out is None) == (dk is None):
+        raise Lite3rError(f"{what}: k, dk_out and dk go together")
+    tensors = [_rows_of_heads(x, q, what) if x is not None else None for x in (q, k, dq_out, dk_out, dq, dk)]
+    if not q.shape == dq_out.shape == dq.shape or (k is not None and not k.shape == dk_out.shape == dk.shape):
+        raise Lite3rError(f"{what}: gradients must have their sources' shapes")
+    how = _rope(q, k, norm, q_weight, None, k_weight, None, eps, positions, base, what)
+    grads = RopeGrads(*(_vector(x, q.shape[3], what) for x in (dq_weight, dq_bias, dk_weight, dk_bias)))
+    _check(lib().lite3r_qk_norm_rope_backward(tensors[0], tensors[1], tensors[2], tensors[3], how, tensors[4], tensors[5], grads,
+                                              workspace.data_ptr(), _bytes_of(workspace, what), _stream_ptr(stream)), what)
+
+
+# ----------------------------------------------------------------------------- microscaled formats and the layers on them
+@dataclass
+class MxTensor:
+    """A microscaled matrix [rows, cols]: blocks of 32 values along a row with one scale 2^(byte - 127)."""
+    codes: torch.Tensor  # uint8 [rows, cols] (mxfp8) or [rows, cols / 2] (mxfp4, even columns in the low halves)
+    scales: torch.Tensor  # uint8 [ceil(rows / 128), ceil(cols / 128), 32, 4, 4]: [r / 128, j / 4, r % 32, r % 128 / 32, j % 4]
+    rows: int
+    cols: int
+    format: str = "mxfp4"
+
+    def check(self, what: str, cols=None, format=None) -> int:
+        """The format's code; raises where the buffers are not those of such a matrix."""
+        if self.format not in MX_FORMATS or (format is not None and self.format != format):
+            raise Lite3rError(f"{what}: microscaled format must be {format or ' or '.join(MX_FORMATS)}")
+        codes, scales = lite3r_mx_sizes(self.format, self.rows, self.cols)
+        for x, size in ((self.codes, codes), (self.scales, scales)):
+            if x.dtype != torch.uint8 or not x.is_contiguous() or x.numel() != size:
+                raise Lite3rError(f"{what}: codes and scales must be contiguous uint8 tensors of a [{self.rows}, {self.cols}] matrix")
+        if cols is not None and cols != self.cols:
+            raise Lite3rError(f"{what}: operands disagree about d_in")
+        return MX_FORMATS[self.format]
+
+
+def lite3r_mx_sizes(format: str, rows: int, cols: int):
+    """Bytes of the codes and of the scales of a microscaled matrix."""
+    if format not in MX_FORMATS:
+        raise Lite3rError(f"lite3r_mx_sizes: microscaled format must be {' or '.join(MX_FORMATS)}")
+    a, b = C.c_size_t(), C.c_size_t()
+    _check(lib().lite3r_mx_sizes(MX_FORMATS[format], rows, cols, C.byref(a), C.byref(b)), "lite3r_mx_sizes")
+    return a.value, b.value
+
+
+def alloc_mx(rows: int, cols: int, format: str, device) -> MxTensor:
+    lite3r_mx_sizes(format, rows, cols)  # refuses what has no such form
+    return MxTensor(torch.empty((rows, cols if format == "mxfp8" else cols // 2), dtype=torch.uint8, device=device),
+                    torch.empty((-(-rows // 128), -(-cols // 128), 32, 4, 4), dtype=torch.uint8, device=device), rows, cols, format)
+
+
+def _matrix(x, what: str, dtypes=OUT_DTYPES) -> int:
+    if x.dim() != 2 or x.stride(1) != 1 or x.dtype not in dtypes:
+        names = " / ".join(str(t).replace("torch.", "") for t in dtypes)
+        raise Lite3rError(f"{what}: matrices must be {names} with contiguous columns")
+    return OUT_DTYPES[x.dtype]
+
+
+def lite3r_quantize_mx(x: torch.Tensor, format: str = "mxfp4", out=None, stream=None) -> MxTensor:
+    """Microscaled form of a CUDA matrix [rows, cols] (fp32 / bf16 / fp16, contiguous columns, cols a multiple of 32):
+    "mxfp4" for operands of lite3r_linear_mxfp4, "mxfp8" for activations kept for the backward pass.  out: an MxTensor to fill."""
+    what = "lite3r_quantize_mx"
+    dtype = _matrix(x, what)
+    rows, cols = x.shape
+    _on_current_device(what, x)
+    if out is None:
+        with torch.cuda.stream(stream):  # memory that belongs to the stream that fills it
+            out = alloc_mx(rows, cols, format, x.device)
+    elif (out.rows, out.cols, out.format) != (rows, cols, format):
+        raise Lite3rError(f"{what}: out has another shape or format")
+    code = out.check(what)
+    _on_current_device(what, out.codes, out.scales)
+    _check(lib().lite3r_quantize_mx(x.data_ptr(), dtype, x.stride(0), rows, cols, code, out.codes.data_ptr(),
+                                    out.scales.data_ptr(), _stream_ptr(stream)), what)
+    return out
+
+
+def lite3r_dequantize_mx(t: MxTensor, out: torch.Tensor, stream=None) -> torch.Tensor:
+    """The values that `t` stands for, into `out` (CUDA [rows, cols] fp32 / bf16 / fp16), which is returned."""
+    what = "lite3r_dequantize_mx"
+    dtype, code = _matrix(out, what), t.check(what)
+    _on_current_device(what, out, t.codes, t.scales)
+    if tuple(out.shape) != (t.rows, t.cols):
+        raise Lite3rError(f"{what}: out must be [{t.rows}, {t.cols}]")
+    _check(lib().lite3r_dequantize_mx(t.codes.data_ptr(), t.scales.data_ptr(), code, t.rows, t.cols, out.data_ptr(), dtype,
+                                      out.stride(0), _stream_ptr(stream)), what)
+    return out
+
+
+def lite3r_linear_mxfp4(x: MxTensor, w: MxTensor, bias, y: torch.Tensor, device_status=None, stream=None) -> None:
+    """y = Q(x) Q(W)^T + b on MXFP4 operands ([rows, d_in] x [d_out, d_in]); y: CUDA [rows, d_out] fp32 / bf16 / fp16;
+    bias: fp32 [d_out] or None."""
+    what = "lite3r_linear_mxfp4"
+    dtype = _matrix(y, what)
+    x.check(what, format="mxfp4"), w.check(what, cols=x.cols, format="mxfp4")
+    _on_current_device(what, x.codes, x.scales, w.codes, w.scales, bias, y, device_status)
+    if tuple(y.shape) != (x.rows, w.rows):
+        raise Lite3rError(f"{what}: y must be [{x.rows}, {w.rows}]")
+    _check(lib().lite3r_linear_mxfp4(x.codes.data_ptr(), x.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(),
+                                     _vector(bias, w.rows, what), x.rows, x.cols, w.rows, y.data_ptr(), dtype, y.stride(0),
+                                     device_status.data_ptr() if device_status is not None else None, _stream_ptr(stream)), what)
+
+
+def lite3r_linear_mx_workspace(rows: int, d_in: int, d_out: int) -> int:
+    a = C.c_size_t()
+    _check(lib().lite3r_linear_mx_workspace(rows, d_in, d_out, C.byref(a)), "lite3r_linear_mx_workspace")
+    return a.value
+
+
+def lite3r_linear_mx_dgrad(dy: torch.Tensor, w: MxTensor, dx: torch.Tensor, device_status=None, stream=None) -> None:
+    """dx = dy . Q(W): gradient of a linear layer's input through its microscaled weight [d_out, d_in].  dy: CUDA bf16
+    [rows, d_out]; dx: CUDA [rows, d_in] fp32 / bf16 / fp16."""
+    what = "lite3r_linear_mx_dgrad"
+    _matrix(dy, what, (torch.bfloat16,))
+    dtype, code = _matrix(dx, what), w.check(what)
+    _on_current_device(what, dy, w.codes, w.scales, dx, device_status)
+    if dy.shape[1] != w.rows or tuple(dx.shape) != (dy.shape[0], w.cols):
+        raise Lite3rError(f"{what}: dy must be [rows, {w.rows}] and dx [rows, {w.cols}]")
+    _check(lib().lite3r_linear_mx_dgrad(dy.data_ptr(), dy.stride(0), w.codes.data_ptr(), w.scales.data_ptr(), code, dy.shape[0],
+                                        w.cols, w.rows, dx.data_ptr(), dtype, dx.stride(0),
+                                        device_status.data_ptr() if device_status is not None else None, _stream_ptr(stream)), what)
+
+
+def lite3r_linear_mx_wgrad(dy: torch.Tensor, x: MxTensor, dw: torch.Tensor, db, workspace: torch.Tensor, device_status=None,
+                           stream=None) -> None:
+    """dw = dy^T . C(x) (CUDA fp32 [d_out, d_in], contiguous) and db = sum of dy over the rows (fp32 [d_out], or None) from
+    the kept form C(x) of the layer's input [rows, d_in].  workspace: lite3r_linear_mx_workspace(rows, d_in, d_out) bytes."""
+    what = "lite3r_linear_mx_wgrad"
+    _matrix(dy, what, (torch.bfloat16,))
+    code = x.check(what)
+    _on_current_device(what, dy, x.codes, x.scales, dw, db, workspace, device_status)
+    if dy.shape[0] != x.rows or dw.dtype != torch.float32 or not dw.is_contiguous() or tuple(dw.shape) != (dy.shape[1], x.cols):
+        raise Lite3rError(f"{what}: dy must be [{x.rows}, d_out] and dw contiguous float32 [d_out, {x.cols}]")
+    _check(lib().lite3r_linear_mx_wgrad(dy.data_ptr(), dy.stride(0), x.codes.data_ptr(), x.scales.data_ptr(), code, x.rows, x.cols,
+                                        dy.shape[1], dw.data_ptr(), _vector(db, dy.shape[1], what), workspace.data_ptr(),
+                                        _bytes_of(workspace, what), device_status.data_ptr() if device_status is not None else None,
+                                        _stream_ptr(stream)), what)
 
 
 # ----------------------------------------------------------------------------- training side of the projection

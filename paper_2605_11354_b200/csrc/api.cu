@@ -600,6 +600,214 @@ lite3r_status lite3r_qkv_project_fp8(const unsigned char* x_codes, const float* 
   return launch_qkv_project(x_codes, x_scales, w_codes, w_scales, bias, *shape, d_model, out, device_status, cs);
 }
 
+static bool float_type(lite3r_dtype t) { return t == LITE3R_F32 || t == LITE3R_BF16 || t == LITE3R_F16; }
+
+// The tensor-map cache allocates on a thread's first call: nothing is thrown through the C boundary.
+extern "C++" {
+template <typename Fn>
+static lite3r_status no_throw(const Fn& fn) {
+  try {
+    return fn();
+  } catch (...) {
+    return record_cuda(cudaErrorMemoryAllocation);
+  }
+}
+}
+
+static lite3r_status check_rope(const lite3r_rope* how) {
+  if (how == nullptr || how->batch <= 0 || how->q_heads <= 0 || how->k_heads < 0 || how->tokens <= 0) return LITE3R_ERR_INVALID_ARG;
+  if (how->q_heads > 0x7FFFFFFF - how->k_heads) return LITE3R_ERR_UNSUPPORTED;
+  if (how->head_dim != 32 && how->head_dim != 64 && how->head_dim != 128 && how->head_dim != 256) return LITE3R_ERR_UNSUPPORTED;
+  if (how->norm != LITE3R_NORM_NONE && how->norm != LITE3R_NORM_RMS && how->norm != LITE3R_NORM_LAYER) return LITE3R_ERR_UNSUPPORTED;
+  if (how->axes < 0 || how->axes > 2) return LITE3R_ERR_UNSUPPORTED;
+  if (!(how->eps >= 0.f) || std::isinf(how->eps)) return LITE3R_ERR_INVALID_ARG;
+  for (const float* p : {how->q_weight, how->q_bias, how->k_weight, how->k_bias})
+    if (!aligned(p, 16)) return LITE3R_ERR_INVALID_ARG;
+  if (how->axes > 0) {
+    if (how->positions == nullptr || !aligned(how->positions, 4) || how->position_stride_b < 0 || how->position_stride_n < 0)
+      return LITE3R_ERR_INVALID_ARG;
+    if (!(how->base > 0.0) || std::isinf(how->base)) return LITE3R_ERR_INVALID_ARG;
+  }
+  return LITE3R_OK;
+}
+
+// A source (strides may be 0) or a result, whose rows must not overlap: sorted by stride, each dimension steps over all of the
+// one before.
+static lite3r_status check_rope_tensor(const lite3r_tensor* x, lite3r_dtype dtype, const lite3r_rope& how, int heads, bool result) {
+  if (x == nullptr || x->ptr == nullptr || !aligned(x->ptr, 16)) return LITE3R_ERR_INVALID_ARG;
+  if (!float_type(x->dtype) || x->dtype != dtype) return LITE3R_ERR_UNSUPPORTED;
+  struct Dim {
+    long long stride, extent;
+  } dims[3] = {{x->stride_b, how.batch}, {x->stride_h, heads}, {x->stride_n, how.tokens}};
+  for (const Dim& d : dims)
+    if (d.stride < 0 || (d.stride % 8)) return LITE3R_ERR_INVALID_ARG;
+  if (!result) return LITE3R_OK;
+  std::sort(dims, dims + 3, [](const Dim& a, const Dim& b) { return a.stride < b.stride; });
+  long long reach = how.head_dim;  // elements that the dimensions so far span
+  for (const Dim& d : dims) {
+    if (d.extent == 1) continue;
+    if (d.stride < reach) return LITE3R_ERR_INVALID_ARG;
+    if (d.stride > 0x7FFFFFFFFFFFFFFFLL / d.extent) return LITE3R_ERR_UNSUPPORTED;
+    reach = d.stride * (d.extent - 1) + reach;
+  }
+  return LITE3R_OK;
+}
+
+lite3r_status lite3r_qk_norm_rope(const lite3r_tensor* q, const lite3r_tensor* k, const lite3r_rope* how, const lite3r_tensor* q_out,
+                                  const lite3r_tensor* k_out, void* stream) {
+  lite3r_status st = check_rope(how);
+  if (st != LITE3R_OK) return st;
+  if (q == nullptr) return LITE3R_ERR_INVALID_ARG;
+  if ((st = check_rope_tensor(q, q->dtype, *how, how->q_heads, false)) != LITE3R_OK) return st;
+  if ((st = check_rope_tensor(q_out, q->dtype, *how, how->q_heads, true)) != LITE3R_OK) return st;
+  if (how->k_heads > 0) {
+    if ((st = check_rope_tensor(k, q->dtype, *how, how->k_heads, false)) != LITE3R_OK) return st;
+    if ((st = check_rope_tensor(k_out, q->dtype, *how, how->k_heads, true)) != LITE3R_OK) return st;
+  } else if (k != nullptr || k_out != nullptr) {
+    return LITE3R_ERR_INVALID_ARG;
+  }
+  if ((st = check_device()) != LITE3R_OK) return st;
+  return launch_rope(q, k, *how, q_out, k_out, static_cast<cudaStream_t>(stream));
+}
+
+lite3r_status lite3r_qk_norm_rope_workspace(int head_dim, size_t* bytes) {
+  if (bytes == nullptr) return LITE3R_ERR_INVALID_ARG;
+  if (head_dim != 32 && head_dim != 64 && head_dim != 128 && head_dim != 256) return LITE3R_ERR_UNSUPPORTED;
+  *bytes = rope_workspace_bytes(head_dim);
+  return LITE3R_OK;
+}
+
+lite3r_status lite3r_qk_norm_rope_backward(const lite3r_tensor* q, const lite3r_tensor* k, const lite3r_tensor* dq_out,
+                                           const lite3r_tensor* dk_out, const lite3r_rope* how, const lite3r_tensor* dq,
+                                           const lite3r_tensor* dk, const lite3r_rope_grads* grads, void* workspace,
+                                           size_t workspace_bytes, void* stream) {
+  lite3r_status st = check_rope(how);
+  if (st != LITE3R_OK) return st;
+  if (q == nullptr || grads == nullptr) return LITE3R_ERR_INVALID_ARG;
+  if ((st = check_rope_tensor(q, q->dtype, *how, how->q_heads, false)) != LITE3R_OK) return st;
+  if ((st = check_rope_tensor(dq_out, q->dtype, *how, how->q_heads, false)) != LITE3R_OK) return st;
+  if ((st = check_rope_tensor(dq, q->dtype, *how, how->q_heads, true)) != LITE3R_OK) return st;
+  if (how->k_heads > 0) {
+    if ((st = check_rope_tensor(k, q->dtype, *how, how->k_heads, false)) != LITE3R_OK) return st;
+    if ((st = check_rope_tensor(dk_out, q->dtype, *how, how->k_heads, false)) != LITE3R_OK) return st;
+    if ((st = check_rope_tensor(dk, q->dtype, *how, how->k_heads, true)) != LITE3R_OK) return st;
+  } else if (k != nullptr || dk_out != nullptr || dk != nullptr || grads->k_weight != nullptr || grads->k_bias != nullptr) {
+    return LITE3R_ERR_INVALID_ARG;
+  }
+  for (const float* p : {grads->q_weight, grads->q_bias, grads->k_weight, grads->k_bias})
+    if (!aligned(p, 4)) return LITE3R_ERR_INVALID_ARG;
+  if (workspace == nullptr || !aligned(workspace, 256)) return LITE3R_ERR_INVALID_ARG;
+  if (workspace_bytes < rope_workspace_bytes(how->head_dim)) return LITE3R_ERR_WORKSPACE;
+  if ((st = check_device()) != LITE3R_OK) return st;
+  return launch_rope_backward(q, k, dq_out, dk_out, *how, dq, dk, *grads, static_cast<float*>(workspace), static_cast<cudaStream_t>(stream));
+}
+
+static lite3r_status check_mx(lite3r_mx_format format, int rows, int cols) {
+  if (format != LITE3R_MXFP4 && format != LITE3R_MXFP8) return LITE3R_ERR_UNSUPPORTED;
+  if (rows <= 0 || cols <= 0 || rows > 0x7FFFFFFF - 256 || cols > 0x7FFFFFFF - 256) return LITE3R_ERR_INVALID_ARG;
+  return (cols % 32) ? LITE3R_ERR_UNSUPPORTED : LITE3R_OK;
+}
+
+// A matrix in 16 or 32 bits.
+static lite3r_status check_matrix(const void* x, lite3r_dtype dtype, long long row_stride, int cols) {
+  if (!float_type(dtype)) return LITE3R_ERR_UNSUPPORTED;
+  return x == nullptr || !aligned(x, 16) || row_stride < cols || (row_stride % 8) || row_stride > (1LL << 36) ? LITE3R_ERR_INVALID_ARG : LITE3R_OK;
+}
+
+static lite3r_status check_codes(const unsigned char* codes, const unsigned char* scales) {
+  return codes == nullptr || scales == nullptr || !aligned(codes, 16) || !aligned(scales, 16) ? LITE3R_ERR_INVALID_ARG : LITE3R_OK;
+}
+
+lite3r_status lite3r_mx_sizes(lite3r_mx_format format, int rows, int cols, size_t* codes_bytes, size_t* scales_bytes) {
+  const lite3r_status st = check_mx(format, rows, cols);
+  if (st != LITE3R_OK) return st;
+  if (codes_bytes) *codes_bytes = static_cast<size_t>(rows) * (format == LITE3R_MXFP4 ? cols / 2 : cols);
+  if (scales_bytes) *scales_bytes = static_cast<size_t>(ceil_div(rows, 128)) * ceil_div(cols, 128) * 512;
+  return LITE3R_OK;
+}
+
+lite3r_status lite3r_quantize_mx(const void* x, lite3r_dtype dtype, long long row_stride, int rows, int cols, lite3r_mx_format format,
+                                 unsigned char* codes, unsigned char* scales, void* stream) {
+  lite3r_status st = check_mx(format, rows, cols);
+  if (st != LITE3R_OK) return st;
+  if ((st = check_matrix(x, dtype, row_stride, cols)) != LITE3R_OK) return st;
+  if ((st = check_codes(codes, scales)) != LITE3R_OK) return st;
+  if ((st = check_device()) != LITE3R_OK) return st;
+  return launch_mx_quantise(x, static_cast<int>(dtype), row_stride, rows, cols, static_cast<int>(format), codes, scales,
+                            static_cast<cudaStream_t>(stream));
+}
+
+lite3r_status lite3r_dequantize_mx(const unsigned char* codes, const unsigned char* scales, lite3r_mx_format format, int rows, int cols,
+                                   void* out, lite3r_dtype dtype, long long row_stride, void* stream) {
+  lite3r_status st = check_mx(format, rows, cols);
+  if (st != LITE3R_OK) return st;
+  if ((st = check_matrix(out, dtype, row_stride, cols)) != LITE3R_OK) return st;
+  if ((st = check_codes(codes, scales)) != LITE3R_OK) return st;
+  if ((st = check_device()) != LITE3R_OK) return st;
+  return launch_mx_dequantise(codes, scales, rows, cols, static_cast<int>(format), out, static_cast<int>(dtype), row_stride,
+                              static_cast<cudaStream_t>(stream));
+}
+
+lite3r_status lite3r_linear_mxfp4(const unsigned char* x_codes, const unsigned char* x_scales, const unsigned char* w_codes,
+                                  const unsigned char* w_scales, const float* bias, int rows, int d_in, int d_out, void* y,
+                                  lite3r_dtype y_dtype, long long y_stride, int* device_status, void* stream) {
+  lite3r_status st = check_mx(LITE3R_MXFP4, rows, d_in);
+  if (st != LITE3R_OK) return st;
+  if (d_out <= 0 || d_out > 0x7FFFFFFF - 256 || !aligned(bias, 4) || !aligned(device_status, 4)) return LITE3R_ERR_INVALID_ARG;
+  if ((st = check_codes(x_codes, x_scales)) != LITE3R_OK) return st;
+  if ((st = check_codes(w_codes, w_scales)) != LITE3R_OK) return st;
+  if ((st = check_matrix(y, y_dtype, y_stride, d_out)) != LITE3R_OK) return st;
+  if ((st = check_device()) != LITE3R_OK) return st;
+  return no_throw([&] {
+    return launch_linear_mxf4(x_codes, x_scales, w_codes, w_scales, bias, rows, d_in, d_out, y, static_cast<int>(y_dtype), y_stride,
+                              device_status, static_cast<cudaStream_t>(stream));
+  });
+}
+
+lite3r_status lite3r_linear_mx_workspace(int rows, int d_in, int d_out, size_t* bytes) {
+  const lite3r_status st = check_mx(LITE3R_MXFP8, rows, d_in);
+  if (st != LITE3R_OK) return st;
+  if (bytes == nullptr || d_out <= 0 || d_out > 0x7FFFFFFF - 256) return LITE3R_ERR_INVALID_ARG;
+  *bytes = linear_mx_workspace_bytes(rows, d_in, d_out);
+  return LITE3R_OK;
+}
+
+static lite3r_status check_mx_back(const void* dy, long long dy_stride, const unsigned char* codes, const unsigned char* scales,
+                                   lite3r_mx_format format, int rows, int d_in, int d_out, const int* device_status) {
+  lite3r_status st = check_mx(format, rows, d_in);
+  if (st != LITE3R_OK) return st;
+  if (d_out <= 0 || d_out > 0x7FFFFFFF - 256 || !aligned(device_status, 4)) return LITE3R_ERR_INVALID_ARG;
+  if ((st = check_codes(codes, scales)) != LITE3R_OK) return st;
+  return check_matrix(dy, LITE3R_BF16, dy_stride, d_out);
+}
+
+lite3r_status lite3r_linear_mx_dgrad(const void* dy, long long dy_stride, const unsigned char* w_codes, const unsigned char* w_scales,
+                                     lite3r_mx_format format, int rows, int d_in, int d_out, void* dx, lite3r_dtype dx_dtype,
+                                     long long dx_stride, int* device_status, void* stream) {
+  lite3r_status st = check_mx_back(dy, dy_stride, w_codes, w_scales, format, rows, d_in, d_out, device_status);
+  if (st != LITE3R_OK) return st;
+  if ((st = check_matrix(dx, dx_dtype, dx_stride, d_in)) != LITE3R_OK) return st;
+  if ((st = check_device()) != LITE3R_OK) return st;
+  return no_throw([&] {
+    return launch_mx_dgrad(dy, dy_stride, w_codes, w_scales, static_cast<int>(format), rows, d_in, d_out, dx, static_cast<int>(dx_dtype),
+                           dx_stride, device_status, static_cast<cudaStream_t>(stream));
+  });
+}
+
+lite3r_status lite3r_linear_mx_wgrad(const void* dy, long long dy_stride, const unsigned char* x_codes, const unsigned char* x_scales,
+                                     lite3r_mx_format format, int rows, int d_in, int d_out, float* dw, float* db, void* workspace,
+                                     size_t workspace_bytes, int* device_status, void* stream) {
+  lite3r_status st = check_mx_back(dy, dy_stride, x_codes, x_scales, format, rows, d_in, d_out, device_status);
+  if (st != LITE3R_OK) return st;
+  if (dw == nullptr || !aligned(dw, 16) || !aligned(db, 4) || workspace == nullptr || !aligned(workspace, 256)) return LITE3R_ERR_INVALID_ARG;
+  if (workspace_bytes < linear_mx_workspace_bytes(rows, d_in, d_out)) return LITE3R_ERR_WORKSPACE;
+  if ((st = check_device()) != LITE3R_OK) return st;
+  return no_throw([&] {
+    return launch_mx_wgrad(dy, dy_stride, x_codes, x_scales, static_cast<int>(format), rows, d_in, d_out, dw, db,
+                           static_cast<float*>(workspace), device_status, static_cast<cudaStream_t>(stream));
+  });
+}
+
 lite3r_status lite3r_selftest_wait_expiry(int* device_status, unsigned long long limit_ns, void* stream) {
   if (device_status == nullptr || limit_ns == 0 || limit_ns > 1000000000ull) return LITE3R_ERR_INVALID_ARG;
   return launch_wait_expiry_probe(device_status, limit_ns, static_cast<cudaStream_t>(stream));

@@ -253,6 +253,30 @@ lite3r_status launch_qkv_project(const uint8_t* x_codes, const float* x_scales, 
                                  const float* w_scales, const float* bias, const lite3r_shape& s, int d_model,
                                  const lite3r_fp8* out, int* device_status, cudaStream_t stream);
 
+// Norms and position rotation of queries and keys (rope.cu).
+size_t rope_workspace_bytes(int head_dim);
+lite3r_status launch_rope(const lite3r_tensor* q, const lite3r_tensor* k, const lite3r_rope& how, const lite3r_tensor* q_out,
+                          const lite3r_tensor* k_out, cudaStream_t stream);
+lite3r_status launch_rope_backward(const lite3r_tensor* q, const lite3r_tensor* k, const lite3r_tensor* dq_out,
+                                   const lite3r_tensor* dk_out, const lite3r_rope& how, const lite3r_tensor* dq,
+                                   const lite3r_tensor* dk, const lite3r_rope_grads& grads, float* partials, cudaStream_t stream);
+
+// Microscaled formats (mx.cu), the linear layer on them (linear_mx.cu) and its backward pass (linear_mx_back.cu).
+lite3r_status launch_mx_quantise(const void* x, int dtype, long long row_stride, int rows, int cols, int format, uint8_t* codes,
+                                 uint8_t* scales, cudaStream_t stream);
+lite3r_status launch_mx_dequantise(const uint8_t* codes, const uint8_t* scales, int rows, int cols, int format, void* out,
+                                   int dtype, long long row_stride, cudaStream_t stream);
+lite3r_status launch_linear_mxf4(const uint8_t* x_codes, const uint8_t* x_scales, const uint8_t* w_codes, const uint8_t* w_scales,
+                                 const float* bias, int rows, int d_in, int d_out, void* y, int y_dtype, long long y_stride,
+                                 int* device_status, cudaStream_t stream);
+size_t linear_mx_workspace_bytes(int rows, int d_in, int d_out);
+lite3r_status launch_mx_dgrad(const void* dy, long long dy_stride, const uint8_t* w_codes, const uint8_t* w_scales, int format,
+                              int rows, int d_in, int d_out, void* dx, int dx_dtype, long long dx_stride, int* device_status,
+                              cudaStream_t stream);
+lite3r_status launch_mx_wgrad(const void* dy, long long dy_stride, const uint8_t* x_codes, const uint8_t* x_scales, int format,
+                              int rows, int d_in, int d_out, float* dw, float* db, float* workspace, int* device_status,
+                              cudaStream_t stream);
+
 // Training side of the linear-branch projection (train.cu).
 size_t train_workspace_bytes(const lite3r_shape& s);
 lite3r_status launch_mse_distill(const void* student, const void* teacher, int dtype, size_t count, __nv_bfloat16* grad,

@@ -1,0 +1,337 @@
+// The linear layer on microscaled 4-bit operands: y = Q(x) Q(W)^T + b with block-scaled tcgen05 products (e2m1 x e2m1, one
+// scale per 32 elements of K, fp32 accumulation in TMEM).
+// A product of two e2m1 values is a multiple of 1/4 below 2^6 and the scales are powers of two, so the fp32 accumulation is
+// exact but for scales that lie many powers of two apart.
+// Persistent CTAs over tiles of 128 rows x kN columns.  Warp 0 loads (A and B as bytes in rows of 128 = 256 elements of K, 128B
+// swizzle; the scale tiles of both as they lie in memory), warp 1 copies the scales to tensor memory and issues the products
+// into one of two accumulators, warps 4 on are epilogue warpgroups, one per 64 columns, which add the bias, round once and
+// store through shared memory.  The products of the next tile run under the epilogue of this one.
+// Every mbarrier wait is bounded; on expiry the CTA sets *device_status and its roles leave their loops.
+#include <algorithm>
+
+#include "common.cuh"
+#include "sm100.cuh"
+
+namespace lite3r {
+
+namespace {
+
+using namespace sm100;
+
+constexpr int kTileM = 128;
+constexpr int kRowBytes = 128;            // of an operand row in a stage
+constexpr int kStageK = 2 * kRowBytes;    // elements of K in a stage
+constexpr int kScaleTile = 512;           // scales of 128 rows x 128 elements of K
+constexpr int kMaxStages = 5;
+
+template <int kN>
+struct Layout {
+  static constexpr int kGroups = kN / 64;                      // epilogue warpgroups
+  static constexpr int kThreads = 128 + 128 * kGroups;
+  static constexpr int kStages = 5;
+  static constexpr uint32_t kOffB = kTileM * kRowBytes;
+  static constexpr uint32_t kOffSfa = kOffB + kN * kRowBytes;  // two scale tiles of A, two of B
+  static constexpr uint32_t kOffSfb = kOffSfa + 2 * kScaleTile;
+  static constexpr uint32_t kStageBytes = kOffSfb + 2 * kScaleTile;
+  static constexpr uint32_t kOffOut = kStages * kStageBytes;   // staged output, 4 KB per epilogue warp
+  static constexpr uint32_t kOffBias = kOffOut + kGroups * 16384;  // two sets by turns
+  static constexpr uint32_t kOffBar = kOffBias + 2 * kN * 4;
+  static constexpr uint32_t kSmemBytes = kOffBar + 256;
+  // tensor memory: two accumulators, then the scales of a stage for A (two columns groups of four) and B
+  static constexpr uint32_t kSfaCol = 2 * kN, kSfbCol = kSfaCol + 8;
+  static constexpr uint32_t kTmemCols = kN == 64 ? 256 : 512;
+  static_assert(kSfbCol + 8 <= kTmemCols && kStageBytes % 1024 == 0 && kSmemBytes <= 232448, "fits");
+};
+
+struct Bars {
+  uint64_t full[kMaxStages], empty[kMaxStages];
+  uint64_t acc_full[2], acc_empty[2];  // accumulator written (issuer -> epilogue) / read out (epilogue -> issuer)
+  uint32_t tmem_base;
+  int abort;
+};
+
+struct MxParams {
+  const uint8_t* x_scales;
+  const uint8_t* w_scales;
+  const float* bias;  // [d_out] or null
+  int rows, d_in, d_out;
+  int k_tiles;        // scale tiles along K
+  int col_tiles, tiles;
+  int y_dtype;
+  int ragged;         // rows of y end inside 16 bytes
+  void* y;
+  long long y_stride;
+  int* status;
+};
+
+__device__ __forceinline__ void named_barrier_sync(int id, int threads) {
+  asm volatile("bar.sync %0, %1;" ::"r"(id), "r"(threads) : "memory");
+}
+
+template <int kN>
+__global__ void __launch_bounds__(Layout<kN>::kThreads, 1)
+linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                   const __grid_constant__ CUtensorMap map_y, const MxParams p) {
+  using L = Layout<kN>;
+  constexpr int kStages = L::kStages;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  Bars* bars = reinterpret_cast<Bars*>(smem + L::kOffBar);
+  volatile int* abort_flag = &bars->abort;
+  if ((smem_u32(smem) & 1023u) != 0) {
+    if (threadIdx.x == 0 && p.status != nullptr) atomicCAS(p.status, 0, 900);
+    return;
+  }
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int stages_k = (p.d_in + kStageK - 1) / kStageK;
+
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < kStages; ++s) {
+      mbar_init(&bars->full[s], 1);
+      mbar_init(&bars->empty[s], 1);
+    }
+    for (int b = 0; b < 2; ++b) {
+      mbar_init(&bars->acc_full[b], 1);
+      mbar_init(&bars->acc_empty[b], L::kGroups * 4);
+    }
+    bars->abort = 0;
+    mbar_fence_init();
+  }
+  if (warp == 1) {
+    tmem_alloc(&bars->tmem_base, L::kTmemCols);
+    tmem_relinquish();
+  }
+  tc_fence_before();
+  __syncthreads();
+  tc_fence_after();
+  const uint32_t tmem = bars->tmem_base;
+  wait_for_prior_grid();
+  launch_dependents();
+  if (blockIdx.x == 0 && threadIdx.x == 0 && p.status != nullptr) *p.status = 0;
+
+  if (warp == 0) {
+    if (lane == 0) {
+      tma_prefetch_desc(&map_x);
+      tma_prefetch_desc(&map_w);
+      bool ok = true;
+      int kc = 0;
+      for (int tile = blockIdx.x; ok && tile < p.tiles; tile += gridDim.x) {
+        const int row_tile = tile / p.col_tiles, col0 = (tile - row_tile * p.col_tiles) * kN;
+        for (int k = 0; ok && k < stages_k; ++k, ++kc) {
+          const int st = kc % kStages;
+          if (kc >= kStages)
+            ok = mbar_wait_clearing(&bars->empty[st], ((kc - kStages) / kStages) & 1, abort_flag, p.status, 801, 32);
+          if (!ok) break;
+          uint8_t* const dst = smem + st * L::kStageBytes;
+          const int scale_tiles = min(2, p.k_tiles - 2 * k);  // the last stage may have one
+          const uint32_t scale_bytes = static_cast<uint32_t>(scale_tiles) * kScaleTile;
+          mbar_arrive_expect_tx(&bars->full[st], (kTileM + kN) * kRowBytes + 2 * scale_bytes);
+          tma_load_2d(dst, &map_x, &bars->full[st], k * kRowBytes, row_tile * kTileM);
+          tma_load_2d(dst + L::kOffB, &map_w, &bars->full[st], k * kRowBytes, col0);
+          bulk_load(dst + L::kOffSfa, p.x_scales + (static_cast<size_t>(row_tile) * p.k_tiles + 2 * k) * kScaleTile, scale_bytes, &bars->full[st]);
+          bulk_load(dst + L::kOffSfb, p.w_scales + (static_cast<size_t>(col0 / 128) * p.k_tiles + 2 * k) * kScaleTile, scale_bytes, &bars->full[st]);
+        }
+      }
+    }
+  } else if (warp == 1) {
+    if (lane == 0) {
+      const uint64_t a_desc0 = smem_desc(smem_u32(smem), 16, 1024, kSwizzle128);
+      const uint64_t b_desc0 = smem_desc(smem_u32(smem) + L::kOffB, 16, 1024, kSwizzle128);
+      const uint64_t sfa_desc0 = smem_desc(smem_u32(smem) + L::kOffSfa, 16, 128, 0);
+      const uint64_t sfb_desc0 = smem_desc(smem_u32(smem) + L::kOffSfb, 16, 128, 0);
+      const int products = (p.d_in + 63) / 64;
+      bool ok = true;
+      int kc = 0, it = 0;
+      for (int tile = blockIdx.x; ok && tile < p.tiles; tile += gridDim.x, ++it) {
+        const int ab = it & 1;
+        // with tiles of 64 columns the weight's scale tile serves two of them: columns 0 and 1, or 2 and 3
+        const uint32_t sfb_shift = kN == 64 ? 2u * ((tile % p.col_tiles) & 1) : 0u;
+        if (it >= 2) ok = mbar_wait_clearing(&bars->acc_empty[ab], ((it - 2) >> 1) & 1, abort_flag, p.status, 804);
+        tc_fence_after();
+        for (int k = 0; ok && k < stages_k; ++k, ++kc) {
+          const int st = kc % kStages;
+          ok = mbar_wait_clearing(&bars->full[st], (kc / kStages) & 1, abort_flag, p.status, 802);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t off = static_cast<uint64_t>((st * L::kStageBytes) >> 4);
+          const int todo = min(4, products - 4 * k);
+          for (int t = 0; t < (todo + 1) / 2; ++t) {
+            tmem_copy_scales(tmem + L::kSfaCol + 4 * t, sfa_desc0 + off + ((t * kScaleTile) >> 4));
+            tmem_copy_scales(tmem + L::kSfbCol + 4 * t, sfb_desc0 + off + ((t * kScaleTile) >> 4));
+          }
+#pragma unroll
+          for (int kk = 0; kk < 4; ++kk) {
+            if (kk >= todo) break;
+            const uint32_t idesc = (kk & 1) ? instr_desc_mxf4(kTileM, kN, 2) : instr_desc_mxf4(kTileM, kN, 0);
+            mma_mxf4(tmem + ab * kN, a_desc0 + off + ((kk * 32) >> 4), b_desc0 + off + ((kk * 32) >> 4), idesc,
+                     tmem + L::kSfaCol + 4 * (kk >> 1), tmem + L::kSfbCol + 4 * (kk >> 1) + sfb_shift, (k > 0 || kk > 0) ? 1u : 0u);
+          }
+          mma_commit(&bars->empty[st]);
+        }
+        if (ok) mma_commit(&bars->acc_full[ab]);
+      }
+    }
+  } else if (warp >= 4) {
+    const int quarter = warp & 3;
+    const int hh = (warp - 4) >> 2;  // which 64 columns of the tile this warpgroup owns
+    const int tid = threadIdx.x - (4 + hh * 4) * 32;
+    uint8_t* const warp_tile = smem + L::kOffOut + hh * 16384 + quarter * 4096;
+    const uint32_t my_row = smem_u32(warp_tile) + lane * 128;
+    const int swz = lane & 7;
+    const bool wide = p.y_dtype == LITE3R_F32;
+    bool ok = true;
+    int it = 0;
+    for (int tile = blockIdx.x; ok && tile < p.tiles; tile += gridDim.x, ++it) {
+      const int ab = it & 1;
+      const int row_tile = tile / p.col_tiles;
+      const int row0 = row_tile * kTileM, col = (tile - row_tile * p.col_tiles) * kN + hh * 64;
+      const uint32_t acc_addr = tmem + ((static_cast<uint32_t>(quarter) * 32u) << 16) + ab * kN + hh * 64;
+      float* const bia = reinterpret_cast<float*>(smem + L::kOffBias) + ab * kN + hh * 64;
+      if (tid < 64) bia[tid] = (p.bias != nullptr && col + tid < p.d_out) ? __ldg(p.bias + col + tid) : 0.f;
+      named_barrier_sync(1 + hh, 128);
+      ok = mbar_wait_clearing(&bars->acc_full[ab], (it >> 1) & 1, abort_flag, p.status, 803);
+      tc_fence_after();
+      ok = __all_sync(0xFFFFFFFFu, ok);
+      if (!ok) break;
+      auto acc_read_out = [&] {
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->acc_empty[ab]);
+      };
+      if (col >= p.d_out) {
+        acc_read_out();
+        continue;
+      }
+      // The warp stages its 32 rows, 128 bytes at a time, in the layout the store engine reads (128B swizzle); rows and
+      // columns past the output are clipped by the engine, columns at 16 bytes: a ragged end is stored value by value.
+      const bool ragged = p.ragged && col + 64 > p.d_out;
+#pragma unroll 1
+      for (int cb = 0; cb < 64; cb += 32) {
+        uint32_t v[32];
+        tmem_ld32(acc_addr + cb, v);
+        if (wide || cb == 0) {  // what was staged here before has been read by the store engine
+          if (lane == 0) bulk_wait_group_read0();
+          __syncwarp();
+        }
+        tmem_wait_ld();
+        if (cb == 32) acc_read_out();
+#pragma unroll
+        for (int c = 0; c < 32; c += 4) {
+          const float4 b4 = *reinterpret_cast<const float4*>(bia + cb + c);
+          v[c] = __float_as_uint(__uint_as_float(v[c]) + b4.x);
+          v[c + 1] = __float_as_uint(__uint_as_float(v[c + 1]) + b4.y);
+          v[c + 2] = __float_as_uint(__uint_as_float(v[c + 2]) + b4.z);
+          v[c + 3] = __float_as_uint(__uint_as_float(v[c + 3]) + b4.w);
+        }
+        if (ragged) {
+          if (row0 + quarter * 32 + lane < p.rows) {
+            uint8_t* const dst = static_cast<uint8_t*>(p.y) + ((row0 + quarter * 32 + lane) * p.y_stride + col + cb) * (wide ? 4 : 2);
+#pragma unroll
+            for (int c = 0; c < 32; ++c) {
+              if (col + cb + c >= p.d_out) continue;
+              const float f = __uint_as_float(v[c]);
+              if (wide) reinterpret_cast<float*>(dst)[c] = f;
+              else if (p.y_dtype == LITE3R_BF16) reinterpret_cast<__nv_bfloat16*>(dst)[c] = __float2bfloat16_rn(f);
+              else reinterpret_cast<__half*>(dst)[c] = __float2half_rn(f);
+            }
+          }
+          continue;
+        }
+        if (wide) {
+#pragma unroll
+          for (int c = 0; c < 8; ++c) sts128(my_row + ((c ^ swz) << 4), v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+        } else {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            uint32_t w[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const float y0 = __uint_as_float(v[8 * c + 2 * q]), y1 = __uint_as_float(v[8 * c + 2 * q + 1]);
+              if (p.y_dtype == LITE3R_BF16) {
+                __nv_bfloat162 h = __floats2bfloat162_rn(y0, y1);
+                w[q] = *reinterpret_cast<uint32_t*>(&h);
+              } else {
+                __half2 h = __floats2half2_rn(y0, y1);
+                w[q] = *reinterpret_cast<uint32_t*>(&h);
+              }
+            }
+            sts128(my_row + (((cb / 8 + c) ^ swz) << 4), w[0], w[1], w[2], w[3]);
+          }
+        }
+        if (wide || cb == 32) {
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) {
+            if (col + (wide ? cb : 0) < p.d_out) tma_store_2d(&map_y, warp_tile, col + (wide ? cb : 0), row0 + quarter * 32);
+            bulk_commit_group();
+          }
+        }
+      }
+    }
+    bulk_wait_group_read0();  // what is staged stays in place until it has been read
+  }
+
+  tc_fence_before();
+  __syncthreads();
+  linger_after_abort(abort_flag);
+  if (warp == 1) {
+    tc_fence_after();
+    tmem_dealloc(tmem, L::kTmemCols);
+  }
+}
+
+template <int kN>
+lite3r_status launch_tiles(const uint8_t* x_codes, const uint8_t* w_codes, const CUtensorMap& map_y, const MxParams& p, int sms,
+                           cudaStream_t stream) {
+  using L = Layout<kN>;
+  CUtensorMap map_x, map_w;
+  lite3r_status st;
+  const uint64_t pitch = static_cast<uint64_t>(p.d_in) / 2;
+  if ((st = make_tensor_map_2d(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, x_codes, pitch, p.rows, kRowBytes, kTileM,
+                               CU_TENSOR_MAP_SWIZZLE_128B)) != LITE3R_OK) return st;
+  if ((st = make_tensor_map_2d(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, w_codes, pitch, p.d_out, kRowBytes, kN,
+                               CU_TENSOR_MAP_SWIZZLE_128B)) != LITE3R_OK) return st;
+  if ((st = ensure_dynamic_smem(linear_mxf4_kernel<kN>, static_cast<int>(L::kSmemBytes))) != LITE3R_OK) return st;
+  MxParams q = p;
+  q.col_tiles = ceil_div(p.d_out, kN);
+  const long long tiles = static_cast<long long>(q.col_tiles) * ceil_div(p.rows, kTileM);
+  if (tiles > 0x7FFFFFFFLL - 1024) return LITE3R_ERR_UNSUPPORTED;
+  q.tiles = static_cast<int>(tiles);
+  return launch_dependent(linear_mxf4_kernel<kN>, dim3(static_cast<unsigned>(std::min(q.tiles, sms))), L::kThreads,
+                          static_cast<int>(L::kSmemBytes), stream, map_x, map_w, map_y, q);
+}
+
+}  // namespace
+
+lite3r_status launch_linear_mxf4(const uint8_t* x_codes, const uint8_t* x_scales, const uint8_t* w_codes, const uint8_t* w_scales,
+                                 const float* bias, int rows, int d_in, int d_out, void* y, int y_dtype, long long y_stride,
+                                 int* device_status, cudaStream_t stream) {
+  int sms = 0;
+  lite3r_status st = sm_count(&sms);
+  if (st != LITE3R_OK) return st;
+  MxParams p = {};
+  p.x_scales = x_scales;
+  p.w_scales = w_scales;
+  p.bias = bias;
+  p.rows = rows;
+  p.d_in = d_in;
+  p.d_out = d_out;
+  p.k_tiles = ceil_div(d_in, 128);
+  p.y_dtype = y_dtype;
+  p.status = device_status;
+  const int elem = y_dtype == LITE3R_F32 ? 4 : 2;
+  p.ragged = (d_out * static_cast<long long>(elem)) % 16 != 0;
+  p.y = y;
+  p.y_stride = y_stride;
+  CUtensorMap map_y;
+  st = make_tensor_map_2d(&map_y,
+                          y_dtype == LITE3R_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                          : y_dtype == LITE3R_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
+                                                   : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
+                          elem, y, d_out, rows, 128 / elem, 32, CU_TENSOR_MAP_SWIZZLE_128B, static_cast<uint64_t>(y_stride) * elem);
+  if (st != LITE3R_OK) return st;
+  return static_cast<long long>(ceil_div(d_out, 128)) * ceil_div(rows, kTileM) < sms
+             ? launch_tiles<64>(x_codes, w_codes, map_y, p, sms, stream)
+             : launch_tiles<128>(x_codes, w_codes, map_y, p, sms, stream);
+}
+
+}  // namespace lite3r
