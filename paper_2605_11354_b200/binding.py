@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+import struct
 from dataclasses import dataclass
 
 import torch
@@ -54,15 +55,10 @@ class Step(C.Structure):
                 ("workspace", C.c_void_p), ("workspace_bytes", C.c_size_t), ("device_status", C.c_void_p)]
 
 
-class Rope(C.Structure):
-    _fields_ = [("batch", C.c_int), ("q_heads", C.c_int), ("k_heads", C.c_int), ("tokens", C.c_int), ("head_dim", C.c_int),
-                ("norm", C.c_int), ("eps", C.c_float), ("q_weight", C.c_void_p), ("q_bias", C.c_void_p),
-                ("k_weight", C.c_void_p), ("k_bias", C.c_void_p), ("axes", C.c_int), ("positions", C.c_void_p),
-                ("position_stride_b", C.c_longlong), ("position_stride_n", C.c_longlong), ("base", C.c_double)]
-
-
-class RopeGrads(C.Structure):
-    _fields_ = [("q_weight", C.c_void_p), ("q_bias", C.c_void_p), ("k_weight", C.c_void_p), ("k_bias", C.c_void_p)]
+# lite3r_tensor, lite3r_rope and lite3r_rope_grads as bytes: packing them takes a third of the time of filling ctypes structures
+TENSOR = struct.Struct("@Pi4xqqq")
+ROPE = struct.Struct("@iiiiiifPPPPiPqqd")
+ROPE_GRADS = struct.Struct("@PPPP")
 
 
 EXPORTS = ("lite3r_fp8_sizes", "lite3r_plan_sizes", "lite3r_forward_workspace", "lite3r_quantize_fp8",
@@ -142,11 +138,11 @@ def lib() -> C.CDLL:
     L.lite3r_proj_lin_backward.argtypes = [C.c_void_p, C.c_void_p, C.POINTER(Shape), C.c_void_p, C.c_void_p, C.c_size_t,
                                            C.c_void_p, C.c_void_p]
     L.lite3r_proj_lin_backward.restype = C.c_int
-    tp, vp, ll = C.POINTER(Tensor), C.c_void_p, C.c_longlong
+    vp, ll = C.c_void_p, C.c_longlong
     for name, argtypes in {
-            "lite3r_qk_norm_rope": [tp, tp, C.POINTER(Rope), tp, tp, vp],
+            "lite3r_qk_norm_rope": [vp, vp, vp, vp, vp, vp],
             "lite3r_qk_norm_rope_workspace": [C.c_int, sz],
-            "lite3r_qk_norm_rope_backward": [tp, tp, tp, tp, C.POINTER(Rope), tp, tp, C.POINTER(RopeGrads), vp, C.c_size_t, vp],
+            "lite3r_qk_norm_rope_backward": [vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_size_t, vp],
             "lite3r_mx_sizes": [C.c_int, C.c_int, C.c_int, sz, sz],
             "lite3r_quantize_mx": [vp, C.c_int, ll, C.c_int, C.c_int, C.c_int, vp, vp, vp],
             "lite3r_dequantize_mx": [vp, vp, C.c_int, C.c_int, C.c_int, vp, C.c_int, ll, vp],
@@ -467,10 +463,12 @@ def lite3r_qkv_project_fp8(x_codes, x_scales, w_codes, w_scales, bias, shape: Sh
 # ----------------------------------------------------------------------------- norms and rotation of queries and keys
 def _on_current_device(what: str, *tensors) -> None:
     """Kernels run on the current device: every tensor (None: not given) has to be there."""
-    current = torch.cuda.current_device() if torch.cuda.is_initialized() else None
+    device = tensors[0].get_device()  # of the host: -1
     for x in tensors:
-        if x is not None and (not x.is_cuda or x.device.index != current):
-            raise Lite3rError(f"{what}: tensors must be on the current CUDA device")
+        if x is not None and x.get_device() != device:
+            device = -1
+    if device < 0 or device != torch._C._cuda_getDevice():
+        raise Lite3rError(f"{what}: tensors must be on the current CUDA device")
 
 
 def _bytes_of(workspace, what: str) -> int:
@@ -480,38 +478,51 @@ def _bytes_of(workspace, what: str) -> int:
     return workspace.numel() * workspace.element_size()
 
 
-def _rows_of_heads(x, like, what: str) -> Tensor:
-    if x.dim() != 4 or x.stride(3) != 1 or x.dtype not in OUT_DTYPES:
-        raise Lite3rError(f"{what}: q, k and their results must be float32 / bfloat16 / float16 [B,H,N,D] with contiguous D")
-    if x.dtype != like.dtype or x.shape[0] != like.shape[0] or x.shape[2:] != like.shape[2:]:
-        raise Lite3rError(f"{what}: one dtype, batch, number of tokens and head dimension for all tensors")
-    return Tensor(x.data_ptr(), OUT_DTYPES[x.dtype], x.stride(0), x.stride(1), x.stride(2))
+def _rows_of_heads(x, dtype, shape, what: str) -> bytes:
+    """lite3r_tensor of a [B,H,N,D] tensor that has to be of this dtype and shape."""
+    b, h, n, d = x.stride() if x.dim() == 4 else (0, 0, 0, 0)
+    if d != 1:
+        raise Lite3rError(f"{what}: q, k and their results must be [B,H,N,D] with contiguous D")
+    if x.dtype != dtype or x.shape != shape:
+        raise Lite3rError(f"{what}: one dtype, batch, number of tokens and head dimension for all tensors, results and gradients "
+                          "of their sources' shapes")
+    return TENSOR.pack(x.data_ptr(), OUT_DTYPES[dtype], b, h, n)
 
 
-def _vector(x, dim: int, what: str):
+def _vector(x, dim: int, what: str) -> int:
     if x is None:
-        return None
-    if x.dtype != torch.float32 or x.dim() != 1 or x.shape[0] != dim or not x.is_contiguous():
-        raise Lite3rError(f"{what}: weights, biases and their gradients must be contiguous float32 [head_dim]")
+        return 0
+    if x.dtype != torch.float32 or x.dim() != 1 or x.numel() != dim or not x.is_contiguous():
+        raise Lite3rError(f"{what}: weights, biases and their gradients must be contiguous float32 vectors of their dimension")
     return x.data_ptr()
 
 
-def _rope(q, k, norm, q_weight, q_bias, k_weight, k_bias, eps, positions, base, what: str) -> Rope:
+def _rope(q, k, norm, affine, eps, positions, base, what: str):
+    """(lite3r_rope, shape of the queries, shape of the keys)"""
+    if q.dtype not in OUT_DTYPES or q.dim() != 4 or (k is not None and k.dim() != 4):
+        raise Lite3rError(f"{what}: q and k must be float32 / bfloat16 / float16 [B,H,N,D]")
     if norm not in NORM_CODES:
         raise Lite3rError(f"{what}: norm must be one of {', '.join(NORM_CODES)}")
-    batch, heads, tokens, dim = q.shape
-    affine = [_vector(x, dim, what) for x in (q_weight, q_bias, k_weight, k_bias)]
-    axes = stride_b = stride_n = 0
+    shape = q.shape
+    batch, heads, tokens, dim = shape
+    k_heads = k.shape[1] if k is not None else 0
+    axes = stride_b = stride_n = pointer = 0
     if positions is not None:
         p = positions if positions.dim() == 3 else positions[None]  # [N, axes]: shared by the sequences
-        if p.dtype != torch.int32 or p.dim() != 3 or p.shape[0] not in (1, batch) or p.shape[1] != tokens or p.shape[2] not in (1, 2):
+        if p.dim() != 3 or p.dtype != torch.int32:
+            raise Lite3rError(f"{what}: positions must be int32 [B, N, axes] or [N, axes]")
+        entries, length, axes = p.shape
+        if entries not in (1, batch) or length != tokens or axes not in (1, 2):
             raise Lite3rError(f"{what}: positions must be int32 [B, N, axes] or [N, axes] with one or two axes")
-        axes = p.shape[2]
-        if axes == 2 and p.stride(2) != 1:
+        stride_b, stride_n, between = p.stride()
+        if axes == 2 and between != 1:
             raise Lite3rError(f"{what}: a position's two coordinates must lie next to each other")
-        stride_b, stride_n = p.stride(0) if p.shape[0] > 1 else 0, p.stride(1)
-    return Rope(batch, heads, k.shape[1] if k is not None else 0, tokens, dim, NORM_CODES[norm], eps, *affine, axes,
-                positions.data_ptr() if positions is not None else None, stride_b, stride_n, base)
+        if entries == 1:
+            stride_b = 0
+        pointer = p.data_ptr()
+    how = ROPE.pack(batch, heads, k_heads, tokens, dim, NORM_CODES[norm], eps, *(_vector(x, dim, what) for x in affine), axes, pointer,
+                    stride_b, stride_n, base)
+    return how, shape, (batch, k_heads, tokens, dim)
 
 
 def lite3r_qk_norm_rope(q: torch.Tensor, k, q_out: torch.Tensor, k_out, norm: str = "layer", q_weight=None, q_bias=None,
@@ -526,11 +537,12 @@ def lite3r_qk_norm_rope(q: torch.Tensor, k, q_out: torch.Tensor, k_out, norm: st
     _on_current_device(what, q, k, q_out, k_out, q_weight, q_bias, k_weight, k_bias, positions)
     if (k is None) != (k_out is None):
         raise Lite3rError(f"{what}: k and k_out go together")
-    tensors = [_rows_of_heads(x, q, what) if x is not None else None for x in (q, k, q_out, k_out)]
-    if q_out.shape != q.shape or (k is not None and k_out.shape != k.shape):
-        raise Lite3rError(f"{what}: results must have their sources' shapes")
-    how = _rope(q, k, norm, q_weight, q_bias, k_weight, k_bias, eps, positions, base, what)
-    _check(lib().lite3r_qk_norm_rope(tensors[0], tensors[1], how, tensors[2], tensors[3], _stream_ptr(stream)), what)
+    how, q_shape, k_shape = _rope(q, k, norm, (q_weight, q_bias, k_weight, k_bias), eps, positions, base, what)
+    dtype = q.dtype
+    _check(lib().lite3r_qk_norm_rope(_rows_of_heads(q, dtype, q_shape, what),
+                                     _rows_of_heads(k, dtype, k_shape, what) if k is not None else None, how,
+                                     _rows_of_heads(q_out, dtype, q_shape, what),
+                                     _rows_of_heads(k_out, dtype, k_shape, what) if k is not None else None, _stream_ptr(stream)), what)
 
 
 def lite3r_qk_norm_rope_workspace(head_dim: int) -> int:
@@ -551,12 +563,12 @@ def lite3r_qk_norm_rope_backward(q: torch.Tensor, k, dq_out: torch.Tensor, dk_ou
                        dk_bias, positions)
     if not (k is None) == (dk_out is None) == (dk is None):
         raise Lite3rError(f"{what}: k, dk_out and dk go together")
-    tensors = [_rows_of_heads(x, q, what) if x is not None else None for x in (q, k, dq_out, dk_out, dq, dk)]
-    if not q.shape == dq_out.shape == dq.shape or (k is not None and not k.shape == dk_out.shape == dk.shape):
-        raise Lite3rError(f"{what}: gradients must have their sources' shapes")
-    how = _rope(q, k, norm, q_weight, None, k_weight, None, eps, positions, base, what)
-    grads = RopeGrads(*(_vector(x, q.shape[3], what) for x in (dq_weight, dq_bias, dk_weight, dk_bias)))
-    _check(lib().lite3r_qk_norm_rope_backward(tensors[0], tensors[1], tensors[2], tensors[3], how, tensors[4], tensors[5], grads,
+    how, q_shape, k_shape = _rope(q, k, norm, (q_weight, None, k_weight, None), eps, positions, base, what)
+    dtype, dim = q.dtype, q_shape[3]
+    tensors = [_rows_of_heads(x, dtype, q_shape, what) for x in (q, dq_out, dq)]
+    tensors += [_rows_of_heads(x, dtype, k_shape, what) for x in (k, dk_out, dk)] if k is not None else [None] * 3
+    grads = ROPE_GRADS.pack(*(_vector(x, dim, what) for x in (dq_weight, dq_bias, dk_weight, dk_bias)))
+    _check(lib().lite3r_qk_norm_rope_backward(tensors[0], tensors[3], tensors[1], tensors[4], how, tensors[2], tensors[5], grads,
                                               workspace.data_ptr(), _bytes_of(workspace, what), _stream_ptr(stream)), what)
 
 
@@ -574,11 +586,13 @@ class MxTensor:
         """The format's code; raises where the buffers are not those of such a matrix."""
         if self.format not in MX_FORMATS or (format is not None and self.format != format):
             raise Lite3rError(f"{what}: microscaled format must be {format or ' or '.join(MX_FORMATS)}")
-        codes, scales = lite3r_mx_sizes(self.format, self.rows, self.cols)
+        rows, width = self.rows, self.cols
+        codes = rows * (width if self.format == "mxfp8" else width // 2)
+        scales = -(-rows // 128) * -(-width // 128) * 512
         for x, size in ((self.codes, codes), (self.scales, scales)):
             if x.dtype != torch.uint8 or not x.is_contiguous() or x.numel() != size:
-                raise Lite3rError(f"{what}: codes and scales must be contiguous uint8 tensors of a [{self.rows}, {self.cols}] matrix")
-        if cols is not None and cols != self.cols:
+                raise Lite3rError(f"{what}: codes and scales must be contiguous uint8 tensors of a [{rows}, {width}] matrix")
+        if cols is not None and cols != width:
             raise Lite3rError(f"{what}: operands disagree about d_in")
         return MX_FORMATS[self.format]
 
@@ -593,7 +607,8 @@ def lite3r_mx_sizes(format: str, rows: int, cols: int):
 
 
 def alloc_mx(rows: int, cols: int, format: str, device) -> MxTensor:
-    lite3r_mx_sizes(format, rows, cols)  # refuses what has no such form
+    if format not in MX_FORMATS or rows <= 0 or cols <= 0 or cols % 32:
+        lite3r_mx_sizes(format, rows, cols)  # refuses what has no such form
     return MxTensor(torch.empty((rows, cols if format == "mxfp8" else cols // 2), dtype=torch.uint8, device=device),
                     torch.empty((-(-rows // 128), -(-cols // 128), 32, 4, 4), dtype=torch.uint8, device=device), rows, cols, format)
 
@@ -613,8 +628,11 @@ def lite3r_quantize_mx(x: torch.Tensor, format: str = "mxfp4", out=None, stream=
     rows, cols = x.shape
     _on_current_device(what, x)
     if out is None:
-        with torch.cuda.stream(stream):  # memory that belongs to the stream that fills it
+        if stream is None:
             out = alloc_mx(rows, cols, format, x.device)
+        else:
+            with torch.cuda.stream(stream):  # memory that belongs to the stream that fills it
+                out = alloc_mx(rows, cols, format, x.device)
     elif (out.rows, out.cols, out.format) != (rows, cols, format):
         raise Lite3rError(f"{what}: out has another shape or format")
     code = out.check(what)

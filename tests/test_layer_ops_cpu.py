@@ -123,13 +123,17 @@ P = 1 << 20  # stands for a device pointer; nothing is launched
 
 
 def source(stride_b=4096, stride_h=64, stride_n=128, dtype=1, ptr=P):
-    return lt.Tensor(ptr, dtype, stride_b, stride_h, stride_n)
+    return lt.TENSOR.pack(ptr or 0, dtype, stride_b, stride_h, stride_n)
 
 
 def how(**change):
-    fields = dict(batch=2, q_heads=2, k_heads=2, tokens=8, head_dim=64, norm=2, eps=1e-5, q_weight=None, q_bias=None,
-                  k_weight=None, k_bias=None, axes=2, positions=P, position_stride_b=16, position_stride_n=2, base=100.0)
-    return lt.Rope(**{**fields, **change})
+    fields = dict(batch=2, q_heads=2, k_heads=2, tokens=8, head_dim=64, norm=2, eps=1e-5, q_weight=0, q_bias=0,
+                  k_weight=0, k_bias=0, axes=2, positions=P, position_stride_b=16, position_stride_n=2, base=100.0)
+    return lt.ROPE.pack(*(x or 0 for x in {**fields, **change}.values()))
+
+
+def grads(q_weight=None, q_bias=None, k_weight=None, k_bias=None):
+    return lt.ROPE_GRADS.pack(q_weight or 0, q_bias or 0, k_weight or 0, k_bias or 0)
 
 
 @pytest.mark.parametrize("change,status", [
@@ -142,7 +146,7 @@ def how(**change):
 def test_rope_refuses_settings(library, change, status):
     s = source()
     assert library.lite3r_qk_norm_rope(s, s, how(**change), s, s, None) == status
-    back = library.lite3r_qk_norm_rope_backward(s, s, s, s, how(**change), s, s, lt.RopeGrads(), P, 1 << 30, None)
+    back = library.lite3r_qk_norm_rope_backward(s, s, s, s, how(**change), s, s, grads(), P, 1 << 30, None)
     assert back == status
 
 
@@ -155,10 +159,10 @@ def test_rope_refuses_tensors(library, bad, status, as_result):
     """as_result False: allowed as a source (broadcast, overlapping rows), refused as a result."""
     s, h = source(), how()
     assert library.lite3r_qk_norm_rope(s, s, h, s, bad, None) == status
-    assert library.lite3r_qk_norm_rope_backward(s, s, s, s, h, s, bad, lt.RopeGrads(), P, 1 << 30, None) == status
+    assert library.lite3r_qk_norm_rope_backward(s, s, s, s, h, s, bad, grads(), P, 1 << 30, None) == status
     if as_result:
         assert library.lite3r_qk_norm_rope(s, bad, h, s, s, None) == status
-        assert library.lite3r_qk_norm_rope_backward(s, s, s, bad, h, s, s, lt.RopeGrads(), P, 1 << 30, None) == status
+        assert library.lite3r_qk_norm_rope_backward(s, s, s, bad, h, s, s, grads(), P, 1 << 30, None) == status
 
 
 def test_rope_refuses_halves(library):
@@ -169,11 +173,11 @@ def test_rope_refuses_halves(library):
     assert library.lite3r_qk_norm_rope(s, s, None, s, s, None) == INVALID
     back = library.lite3r_qk_norm_rope_backward
     need = lt.lite3r_qk_norm_rope_workspace(64)
-    assert back(s, s, s, s, how(), s, s, lt.RopeGrads(), None, need, None) == INVALID
-    assert back(s, s, s, s, how(), s, s, lt.RopeGrads(), P + 16, need, None) == INVALID
-    assert back(s, s, s, s, how(), s, s, lt.RopeGrads(), P, need - 1, None) == WORKSPACE
+    assert back(s, s, s, s, how(), s, s, grads(), None, need, None) == INVALID
+    assert back(s, s, s, s, how(), s, s, grads(), P + 16, need, None) == INVALID
+    assert back(s, s, s, s, how(), s, s, grads(), P, need - 1, None) == WORKSPACE
     assert back(s, s, s, s, how(), s, s, None, P, need, None) == INVALID
-    assert back(s, None, s, None, how(k_heads=0), s, None, lt.RopeGrads(k_weight=P), P, need, None) == INVALID
+    assert back(s, None, s, None, how(k_heads=0), s, None, grads(k_weight=P), P, need, None) == INVALID
     with pytest.raises(lt.Lite3rError, match="unsupported"):
         lt.lite3r_qk_norm_rope_workspace(96)
 
