@@ -5,10 +5,11 @@
 //                          dx = r (gh - mean(gh) - xh mean(gh xh))   (layer norm; no mean(gh) for the root mean square norm)
 // Both are one pass over the tensors and bound by HBM.  D / 16 lanes work on a row, each on eight pairs: the eight values at i
 // and the eight at i + S/2 (16-byte loads of 16-bit types), so that a rotation needs no other lane and the sums of a row of
-// 64 values take two shuffles.  (Eight lanes to a row, four pairs each: 159 instructions per 256 values instead of
-// KINSTR per 512, and 172 us instead of KFRAME for 32 frames of 16 heads.)  A group of lanes stays with one token and walks its heads
+// 64 values take two shuffles.  A group of lanes stays with one token and walks its heads
 // while the next ones' loads are under way; sine, cosine, weight and bias meet in six coefficients per pair, made once per
 // token.  Arithmetic on packed pairs of fp32.
+// 32 frames of 1374 tokens, 16 heads of 64 bf16 queries and keys: 67 us, 5.4 TB/s (172 us with four pairs to a lane and scalar
+// arithmetic, 159 instructions per 256 values); a hundred frames 188 us, 6.0 TB/s; the gradient of 32 frames 116 us, 4.7 TB/s.
 // Angles: position * base^(-2i/S) / 2 pi in 64-bit fixed point (an fp32 product of a position of a million is off by a tenth of
 // a radian), whose overflow leaves the fraction of a turn; that in fp32.  Sums and norms are fp32; results are rounded once.
 #include <algorithm>
