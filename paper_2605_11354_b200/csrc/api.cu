@@ -804,7 +804,7 @@ lite3r_status lite3r_linear_mx_wgrad(const void* dy, long long dy_stride, const 
   if ((st = check_device()) != LITE3R_OK) return st;
   return no_throw([&] {
     return launch_mx_wgrad(dy, dy_stride, x_codes, x_scales, static_cast<int>(format), rows, d_in, d_out, dw, db,
-                           static_cast<float*>(workspace), device_status, static_cast<cudaStream_t>(stream));
+                           static_cast<float*>(workspace), workspace_bytes, device_status, static_cast<cudaStream_t>(stream));
   });
 }
 

@@ -274,8 +274,8 @@ lite3r_status launch_mx_dgrad(const void* dy, long long dy_stride, const uint8_t
                               int rows, int d_in, int d_out, void* dx, int dx_dtype, long long dx_stride, int* device_status,
                               cudaStream_t stream);
 lite3r_status launch_mx_wgrad(const void* dy, long long dy_stride, const uint8_t* x_codes, const uint8_t* x_scales, int format,
-                              int rows, int d_in, int d_out, float* dw, float* db, float* workspace, int* device_status,
-                              cudaStream_t stream);
+                              int rows, int d_in, int d_out, float* dw, float* db, float* workspace, size_t workspace_bytes,
+                              int* device_status, cudaStream_t stream);
 
 // Training side of the linear-branch projection (train.cu).
 size_t train_workspace_bytes(const lite3r_shape& s);

@@ -4,17 +4,22 @@
 // Both are products C[m][n] = sum_r A(m, r) B[r][n] of bf16 values with codes whose blocks of 32 run along n.  A block's scale
 // is not constant along the contraction, so block-scaled products cannot take it; the codes become bf16 on their way to the
 // tensor cores instead, which is exact (e4m3 and e2m1 have at most four significant bits and the scales are powers of two).
-// Persistent CTAs over tiles of 128 x 256 (wgrad: times a part of the rows).  Warp 0 loads codes and scales, warp 2 the tiles
-// of dy (for wgrad as they lie, the contraction along the rows: M-major), eight warps turn codes into the bf16 operand in
-// shared memory (N-major, 128B swizzle), warp 1 issues the products into one of two accumulators, four warps are the epilogue.
+//
+// Pairs of CTAs (cta_group::2) walk tiles of 256 x 256 or 256 x 128 (wgrad: times a part of the rows): each CTA has 128 rows of A
+// and half of B's columns.  Per CTA: warp 0 loads codes and scales, warp 2 the tiles of dy (for wgrad as they lie, the contraction
+// along the rows: M-major), sixteen warps turn codes into the bf16 operand in shared memory (N-major, 128B swizzle), warp 1 of
+// the pair's first CTA issues the products into one of two accumulators, four warps are the epilogue.
+// The sixteen warps work in four groups, each on every fourth step: a step's chain of load, arithmetic, store and proxy fence
+// takes longer than its products (1900 cycles of a step with all warps on the same one, 512 of products), four chains side by
+// side do not.  Each CTA converts half of B for the pair, about 30 instructions per eight values.  The warps that convert the
+// first column tile's steps of wgrad also add up the columns of dy for db while its tile lies in shared memory.
+//
 // The tensor cores' running sum is cut off, not rounded, at fp32: it drifts towards zero by about 4e-9 of the result per
 // product of 16 steps (10992 rows in one sum: dW off by 2.6e-6).  Results in fp32 are therefore summed over 2048 steps at a time
 // and the sums added with rounding by the store engine, in order, as each is finished.  The parts of the rows that wgrad gives
 // to different CTAs are added in a fixed order by a second kernel: no floating-point atomics between CTAs.
 // Every mbarrier wait is bounded; on expiry the CTA sets *device_status and its roles leave their loops.
 #include <algorithm>
-
-#include <cuda_fp4.h>
 
 #include "common.cuh"
 #include "sm100.cuh"
@@ -25,55 +30,63 @@ namespace {
 
 using namespace sm100;
 
-constexpr int kTileM = 128, kTileN = 256, kTileR = 64;
+constexpr int kTileM = 256, kTileN = 256, kTileR = 64;  // of a pair; a tile may have half the columns
 constexpr int kScaleTile = 512;
-constexpr int kConvWarps = 8;
-constexpr int kThreads = 128 + 32 * kConvWarps + 128;
+constexpr int kGroups = 4, kGroupThreads = 128;          // converting groups
+constexpr int kThreads = 128 + kGroups * kGroupThreads + 128;
 constexpr uint32_t kTmemCols = 512;
 
 template <int kFormat>
 struct Layout {
-  static constexpr int kRaw = 3, kOps = 3;                       // stages of codes, stages of operands
-  static constexpr int kRowBytes = kFormat == LITE3R_MXFP8 ? kTileN : kTileN / 2;
-  static constexpr uint32_t kOffB = kTileM * kTileR * 2;         // A, then B as four boxes of 64 columns x 64 rows
-  static constexpr uint32_t kOpBytes = kOffB + kTileN * kTileR * 2;
+  static constexpr int kRaw = 5, kOps = 5;                      // stages of codes, stages of operands
+  static constexpr int kBoxBytes = kFormat == LITE3R_MXFP8 ? 64 : 32;  // of 64 columns of codes
+  static constexpr uint32_t kOffB = 128 * kTileR * 2;           // A, then B as two boxes of 64 columns x 64 rows
+  static constexpr uint32_t kOpBytes = kOffB + 128 * kTileR * 2;
   static constexpr uint32_t kOffRaw = kOps * kOpBytes;
-  static constexpr uint32_t kOffScales = kTileR * kRowBytes;     // of a raw stage: two scale tiles
-  static constexpr uint32_t kRawBytes = kOffScales + 2 * kScaleTile;
-  static constexpr uint32_t kOffOut = kOffRaw + kRaw * kRawBytes;  // 4 KB per epilogue warp
+  static constexpr uint32_t kOffScales = 2 * kTileR * kBoxBytes;  // of a raw stage: two boxes of codes, one scale tile
+  static constexpr uint32_t kRawBytes = kOffScales + kScaleTile;
+  static constexpr uint32_t kOffOut = (kOffRaw + kRaw * kRawBytes + 1023) / 1024 * 1024;  // 4 KB per epilogue warp
   static constexpr uint32_t kOffBar = kOffOut + 4 * 4096;
-  static constexpr uint32_t kSmemBytes = kOffBar + 256;
-  static_assert(kOffOut % 1024 == 0 && kSmemBytes <= 232448, "fits");
+  static constexpr uint32_t kSmemBytes = kOffBar + 512;
+  static_assert(kSmemBytes <= 232448, "fits");
 };
 
 struct Bars {
-  uint64_t raw_full[3], raw_empty[3], a_full[3], b_full[3], op_empty[3];
-  uint64_t acc_full[2], acc_empty[2];
+  uint64_t raw_full[5], raw_empty[5], a_full[5], op_empty[5];
+  uint64_t b_full[5];                   // of the first CTA: both CTAs' operands are there
+  uint64_t acc_full[2], acc_empty[2];   // acc_empty: of the first CTA
   uint32_t tmem_base;
   int abort;
 };
 
 struct BackParams {
   const uint8_t* scales;
-  int n_total;               // d_in
-  int scale_tiles;           // along n
-  int steps, steps_per_part; // of 64 along the contraction, in all and of one part of it
-  int steps_per_sum;         // of one running sum in tensor memory
-  int col_tiles, tiles, units;
+  float* bias_parts;          // wgrad: [parts][groups][4 warps][m_total], or null
+  int m_total, n_total;       // rows and columns of the result
+  int scale_tiles;            // along n
+  int steps, steps_per_part;  // of 64 along the contraction, in all and of one part of it
+  int steps_per_sum;          // of one running sum in tensor memory
+  int wide_tiles, half_tiles; // columns of a row of tiles: those of 256 first, then those of 128
+  int row_tiles, parts, units;
   int out_dtype;
   int* status;
 };
 
-// bf16 pairs of four codes (eight bits each) or eight (four bits each) without their block's scale: values times 2^-120
-// (e4m3) or as they are (e2m1).
+__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
+  const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
+  return *reinterpret_cast<const uint32_t*>(&r);
+}
+
+// Eight codes of a row to bf16 pairs.  A code's sign goes to bit 15, its exponent behind bf16's bias and its mantissa on top of
+// seven bits: that is the value times 2^-kBias (denormals included), which the block's factor 2^(byte - 127 + kBias) undoes.
 template <int kFormat>
 struct Codes;
 template <>
 struct Codes<LITE3R_MXFP8> {
   static constexpr int kBias = 120;
   uint2 w;
-  __device__ __forceinline__ void load(const uint8_t* raw, int chunk) { w = *(reinterpret_cast<const uint2*>(raw) + chunk); }
-  // sign to bit 15, the four exponent bits behind bf16's bias, three mantissa bits on top of seven
+  __device__ __forceinline__ void load(const uint8_t* at) { w = *reinterpret_cast<const uint2*>(at); }
+  static constexpr int kBytes = 8;
   static __device__ __forceinline__ uint32_t spread(uint32_t pair) { return ((pair >> 4) & 0x07F007F0u) | (pair & 0x80008000u); }
   __device__ __forceinline__ void pairs(uint32_t out[4]) const {
     out[0] = spread(__byte_perm(w.x, 0u, 0x1404));
@@ -84,38 +97,30 @@ struct Codes<LITE3R_MXFP8> {
 };
 template <>
 struct Codes<LITE3R_MXFP4> {
-  static constexpr int kBias = 0;
+  static constexpr int kBias = 126;
   uint32_t w;
-  __device__ __forceinline__ void load(const uint8_t* raw, int chunk) { w = *(reinterpret_cast<const uint32_t*>(raw) + chunk); }
-  // the high and low bytes of the eight magnitudes 0, 0.5, 1, 1.5, 2, 3, 4, 6 as bf16, by table
+  __device__ __forceinline__ void load(const uint8_t* at) { w = *reinterpret_cast<const uint32_t*>(at); }
+  static constexpr int kBytes = 4;
+  static __device__ __forceinline__ uint32_t spread(uint32_t pair) { return ((pair >> 6) & 0x01C001C0u) | (pair & 0x80008000u); }
   __device__ __forceinline__ void pairs(uint32_t out[4]) const {
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const uint32_t four = w >> (16 * i), sel = four & 0x7777u;
-      const uint32_t hi = __byte_perm(0x3F3F3F00u, 0x40404040u, sel), lo = __byte_perm(0xC0800000u, 0xC0804000u, sel);
-      out[2 * i] = __byte_perm(lo, hi, 0x5140) | ((four << 12) & 0x8000u) | ((four << 24) & 0x80000000u);
-      out[2 * i + 1] = __byte_perm(lo, hi, 0x7362) | ((four << 4) & 0x8000u) | ((four << 16) & 0x80000000u);
-    }
+    const uint32_t even = w << 4;  // the even columns' codes in the bytes' upper halves, as the odd ones' are in w
+    out[0] = spread(__byte_perm(even, w, 0x4004));  // (what else is in these bytes the masks take away)
+    out[1] = spread(__byte_perm(even, w, 0x5111));
+    out[2] = spread(__byte_perm(even, w, 0x6222));
+    out[3] = spread(__byte_perm(even, w, 0x7333));
   }
 };
 
-__device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
-  const __nv_bfloat162 r = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&a), *reinterpret_cast<const __nv_bfloat162*>(&b));
-  return *reinterpret_cast<const uint32_t*>(&r);
-}
-// 2^(byte - 127 + kBias) as a pair of bf16; the byte 0xFF stands for NaN.  Where that is beyond bf16's largest power the
-// factor is made of two.
-template <int kBias>
+// kFar: some factor of the warp's blocks is beyond bf16's largest power (or NaN) and is made of two.
+template <int kBias, bool kFar>
 __device__ __forceinline__ void scale_pairs(uint32_t v[4], uint32_t byte) {
-  uint32_t e = byte + kBias;
-  if (e > 254u) {
+  uint32_t f = (byte + kBias) << 7;
+  if constexpr (kFar) {
     constexpr uint32_t kFirst = (static_cast<uint32_t>(kBias) + 127u) << 7;
 #pragma unroll
     for (int i = 0; i < 4; ++i) v[i] = mul_bf16x2(v[i], kFirst | kFirst << 16);
-    e = byte;
+    f = byte == 0xFFu ? 0x7FC0u : byte == 0u ? 0x0040u : byte << 7;
   }
-  uint32_t f = e == 0u ? 0x0040u : e << 7;
-  if (byte == 0xFFu) f = 0x7FC0u;
   f |= f << 16;
 #pragma unroll
   for (int i = 0; i < 4; ++i) v[i] = mul_bf16x2(v[i], f);
@@ -130,34 +135,36 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
   extern __shared__ __align__(1024) uint8_t smem[];
   Bars* bars = reinterpret_cast<Bars*>(smem + L::kOffBar);
   volatile int* abort_flag = &bars->abort;
-  if ((smem_u32(smem) & 1023u) != 0) {
+  if ((smem_u32(smem) & 1023u) != 0) {  // the same in both CTAs of a pair
     if (threadIdx.x == 0 && p.status != nullptr) atomicCAS(p.status, 0, 900);
     return;
   }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int rank = static_cast<int>(cluster_rank());
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kRaw; ++s) {
       mbar_init(&bars->raw_full[s], 1);
-      mbar_init(&bars->raw_empty[s], kConvWarps);
+      mbar_init(&bars->raw_empty[s], kGroupThreads / 32);
     }
     for (int s = 0; s < kOps; ++s) {
       mbar_init(&bars->a_full[s], 1);
-      mbar_init(&bars->b_full[s], kConvWarps);
       mbar_init(&bars->op_empty[s], 1);
+      mbar_init(&bars->b_full[s], 2 * kGroupThreads / 32);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&bars->acc_full[b], 1);
-      mbar_init(&bars->acc_empty[b], 4);
+      mbar_init(&bars->acc_empty[b], 8);
     }
     bars->abort = 0;
     mbar_fence_init();
   }
   if (warp == 1) {
-    tmem_alloc(&bars->tmem_base, kTmemCols);
-    tmem_relinquish();
+    tmem_alloc_pair(&bars->tmem_base, kTmemCols);
+    tmem_relinquish_pair();
   }
   tc_fence_before();
+  cluster_sync();  // barriers and tensor memory of both CTAs are there
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bars->tmem_base;
@@ -165,37 +172,50 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
   launch_dependents();
   if (blockIdx.x == 0 && threadIdx.x == 0 && p.status != nullptr) *p.status = 0;
 
+  // Units: the wide tiles of all parts, then the halves.
+  const int wide_units = p.wide_tiles * p.row_tiles * p.parts;
   struct UnitAt {
-    int m0, n0, part, first, last;  // steps [first, last) of the contraction
+    int m0, n0, part, first, last;  // this CTA's rows, the pair's columns, steps [first, last) of the contraction
+    bool half;
   };
   auto unit_at = [&](int unit) {
     UnitAt u;
-    u.part = kWgrad ? unit / p.tiles : 0;
-    const int tile = unit - u.part * p.tiles, row_tile = tile / p.col_tiles;
-    u.m0 = row_tile * kTileM;
-    u.n0 = (tile - row_tile * p.col_tiles) * kTileN;
+    u.half = unit >= wide_units;
+    if (u.half) unit -= wide_units;
+    const int cols = u.half ? p.half_tiles : p.wide_tiles;
+    const int per_part = cols * p.row_tiles;
+    u.part = kWgrad ? unit / per_part : 0;
+    const int tile = unit - u.part * per_part, row_tile = tile / cols, col = tile - row_tile * cols;
+    u.m0 = row_tile * kTileM + rank * 128;
+    u.n0 = u.half ? p.wide_tiles * kTileN + col * (kTileN / 2) : col * kTileN;
     u.first = u.part * p.steps_per_part;
     u.last = min(u.first + p.steps_per_part, p.steps);
     return u;
   };
+  const int first_unit = blockIdx.x >> 1, unit_step = gridDim.x >> 1;
 
   if (warp == 0) {
     if (lane == 0) {
       tma_prefetch_desc(&map_codes);
       bool ok = true;
       int kc = 0;
-      for (int unit = blockIdx.x; ok && unit < p.units; unit += gridDim.x) {
+      for (int unit = first_unit; ok && unit < p.units; unit += unit_step) {
         const UnitAt u = unit_at(unit);
-        const int scale_tiles = min(2, p.scale_tiles - u.n0 / 128);
+        const int n = u.n0 + rank * (u.half ? 64 : 128);  // this CTA's columns
+        const bool scales = n / 128 < p.scale_tiles;      // (none where they are all past the end)
+        const uint32_t bytes = (u.half ? 1 : 2) * kTileR * L::kBoxBytes + (scales ? kScaleTile : 0);
         for (int k = u.first; ok && k < u.last; ++k, ++kc) {
           const int st = kc % kRaw;
           if (kc >= kRaw) ok = mbar_wait_clearing(&bars->raw_empty[st], ((kc - kRaw) / kRaw) & 1, abort_flag, p.status, 811, 32);
           if (!ok) break;
           uint8_t* const dst = smem + L::kOffRaw + st * L::kRawBytes;
-          mbar_arrive_expect_tx(&bars->raw_full[st], kTileR * L::kRowBytes + scale_tiles * kScaleTile);
-          tma_load_2d(dst, &map_codes, &bars->raw_full[st], kFormat == LITE3R_MXFP8 ? u.n0 : u.n0 / 2, k * kTileR);
-          bulk_load(dst + L::kOffScales, p.scales + (static_cast<size_t>(k / 2) * p.scale_tiles + u.n0 / 128) * kScaleTile,
-                    scale_tiles * kScaleTile, &bars->raw_full[st]);
+          mbar_arrive_expect_tx(&bars->raw_full[st], bytes);
+          const int x = kFormat == LITE3R_MXFP8 ? n : n / 2;
+          tma_load_2d(dst, &map_codes, &bars->raw_full[st], x, k * kTileR);
+          if (!u.half) tma_load_2d(dst + kTileR * L::kBoxBytes, &map_codes, &bars->raw_full[st], x + L::kBoxBytes, k * kTileR);
+          if (scales)
+            bulk_load(dst + L::kOffScales, p.scales + (static_cast<size_t>(k / 2) * p.scale_tiles + n / 128) * kScaleTile, kScaleTile,
+                      &bars->raw_full[st]);
         }
       }
     }
@@ -204,14 +224,14 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
       tma_prefetch_desc(&map_dy);
       bool ok = true;
       int kc = 0;
-      for (int unit = blockIdx.x; ok && unit < p.units; unit += gridDim.x) {
+      for (int unit = first_unit; ok && unit < p.units; unit += unit_step) {
         const UnitAt u = unit_at(unit);
         for (int k = u.first; ok && k < u.last; ++k, ++kc) {
           const int st = kc % kOps;
           if (kc >= kOps) ok = mbar_wait_clearing(&bars->op_empty[st], ((kc - kOps) / kOps) & 1, abort_flag, p.status, 812, 32);
           if (!ok) break;
           uint8_t* const dst = smem + st * L::kOpBytes;
-          mbar_arrive_expect_tx(&bars->a_full[st], kTileM * kTileR * 2);
+          mbar_arrive_expect_tx(&bars->a_full[st], 128 * kTileR * 2);
           if constexpr (kWgrad) {  // two boxes of 64 columns x 64 rows of dy
             tma_load_2d(dst, &map_dy, &bars->a_full[st], u.m0, k * kTileR);
             tma_load_2d(dst + 8192, &map_dy, &bars->a_full[st], u.m0 + 64, k * kTileR);
@@ -222,79 +242,121 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
-      constexpr uint32_t idesc = instr_desc(1, kTileM, kTileN, kWgrad ? 1 : 0, 1);
+    if (lane == 0 && rank == 0) {
+      constexpr uint32_t idesc_wide = instr_desc(1, kTileM, kTileN, kWgrad ? 1 : 0, 1);
+      constexpr uint32_t idesc_half = instr_desc(1, kTileM, kTileN / 2, kWgrad ? 1 : 0, 1);
       const uint32_t base = smem_u32(smem);
       bool ok = true;
       int kc = 0, it = 0;
-      for (int unit = blockIdx.x; ok && unit < p.units; unit += gridDim.x) {
+      for (int unit = first_unit; ok && unit < p.units; unit += unit_step) {
         const UnitAt u = unit_at(unit);
+        const uint32_t idesc = u.half ? idesc_half : idesc_wide;
         for (int k0 = u.first; ok && k0 < u.last; k0 += p.steps_per_sum, ++it) {
-        const int ab = it & 1, k1 = min(k0 + p.steps_per_sum, u.last);
-        if (it >= 2) ok = mbar_wait_clearing(&bars->acc_empty[ab], ((it - 2) >> 1) & 1, abort_flag, p.status, 814);
-        tc_fence_after();
-        for (int k = k0; ok && k < k1; ++k, ++kc) {
-          const int st = kc % kOps;
-          ok = mbar_wait_clearing(&bars->a_full[st], (kc / kOps) & 1, abort_flag, p.status, 815) &&
-               mbar_wait_clearing(&bars->b_full[st], (kc / kOps) & 1, abort_flag, p.status, 816);
-          if (!ok) break;
+          const int ab = it & 1, k1 = min(k0 + p.steps_per_sum, u.last);
+          if (it >= 2) ok = mbar_wait_clearing(&bars->acc_empty[ab], ((it - 2) >> 1) & 1, abort_flag, p.status, 814);
           tc_fence_after();
-          const uint32_t a = base + st * L::kOpBytes, b = a + L::kOffB;
+          for (int k = k0; ok && k < k1; ++k, ++kc) {
+            const int st = kc % kOps;
+            ok = mbar_wait_cluster_clearing(&bars->b_full[st], (kc / kOps) & 1, abort_flag, p.status, 816);
+            if (!ok) break;
+            tc_fence_after();
+            const uint32_t a = base + st * L::kOpBytes, b = a + L::kOffB;
 #pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {  // 16 steps of the contraction each
-            const uint64_t a_desc = kWgrad ? smem_desc(a + kk * 2048, 8192, 1024, kSwizzle128) : smem_desc(a + kk * 32, 16, 1024, kSwizzle128);
-            mma_f16(tmem + ab * kTileN, a_desc, smem_desc(b + kk * 2048, 8192, 1024, kSwizzle128), idesc, (k > k0 || kk > 0) ? 1u : 0u);
+            for (int kk = 0; kk < 4; ++kk) {  // 16 steps of the contraction each
+              const uint64_t a_desc = kWgrad ? smem_desc(a + kk * 2048, 8192, 1024, kSwizzle128) : smem_desc(a + kk * 32, 16, 1024, kSwizzle128);
+              mma_f16_pair(tmem + ab * kTileN, a_desc, smem_desc(b + kk * 2048, 8192, 1024, kSwizzle128), idesc, (k > k0 || kk > 0) ? 1u : 0u);
+            }
+            mma_commit_pair(&bars->op_empty[st]);
           }
-          mma_commit(&bars->op_empty[st]);
-        }
-        if (ok) mma_commit(&bars->acc_full[ab]);
+          if (ok) mma_commit_pair(&bars->acc_full[ab]);
         }
       }
     }
-  } else if (warp >= 4 && warp < 4 + kConvWarps) {
+  } else if (warp >= 4 && warp < 4 + kGroups * 4) {
     // ------------------------------------------------------------------------------------------ codes to bf16
-    constexpr int kPerRow = kTileN / 8;                            // chunks of eight columns
-    constexpr int kChunks = kTileR * kPerRow / (32 * kConvWarps);  // of a thread
-    const int first = (warp - 4) * 32 + lane;
+    const int group = (warp - 4) >> 2, t = threadIdx.x & (kGroupThreads - 1);
+    const int row = t >> 3, chunk = t & 7;  // of sixteen rows and eight chunks of eight columns at a time
     bool ok = true;
     int kc = 0;
-    for (int unit = blockIdx.x; ok && unit < p.units; unit += gridDim.x) {
+    for (int unit = first_unit; ok && unit < p.units; unit += unit_step) {
       const UnitAt u = unit_at(unit);
-      for (int k = u.first; ok && k < u.last; ++k, ++kc) {
-        const int rs = kc % kRaw, st = kc % kOps;
-        ok = mbar_wait_clearing(&bars->raw_full[rs], (kc / kRaw) & 1, abort_flag, p.status, 817);
-        if (ok && kc >= kOps) ok = mbar_wait_clearing(&bars->op_empty[st], ((kc - kOps) / kOps) & 1, abort_flag, p.status, 818);
+      const int block = (u.half ? 2 * rank : 0) + (chunk >> 2);  // of the scale tile's four, for the first box
+      const bool sums = kWgrad && p.bias_parts != nullptr && u.n0 == 0 && u.m0 < p.m_total;
+      float acc[4] = {};  // columns 2 lane, 2 lane + 1 of the two boxes of dy, over this warp's rows
+      const int steps = u.last - u.first;
+      // the first step of the unit that is this group's
+      for (int i = (group - kc % kGroups + kGroups) % kGroups; ok && i < steps; i += kGroups) {
+        const int at = kc + i, k = u.first + i;
+        const int rs = at % kRaw, st = at % kOps;
+        ok = mbar_wait_clearing(&bars->raw_full[rs], (at / kRaw) & 1, abort_flag, p.status, 817);
+        if (ok && at >= kOps) ok = mbar_wait_clearing(&bars->op_empty[st], ((at - kOps) / kOps) & 1, abort_flag, p.status, 818);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
         const uint8_t* const raw = smem + L::kOffRaw + rs * L::kRawBytes;
-        const uint8_t* const scales = raw + L::kOffScales;
-        const uint32_t dst = smem_u32(smem) + st * L::kOpBytes + L::kOffB;
-        Codes<kFormat> c[kChunks];
-        uint32_t byte[kChunks];
+        const uint8_t* const scales = raw + L::kOffScales + ((k & 1) * 2) * 4 + block;
+        const uint32_t dst = smem_u32(smem) + st * L::kOpBytes + L::kOffB + row * 128 + ((chunk ^ (row & 7)) << 4);
+        // two boxes (a half tile: one) of 64 columns, four times sixteen rows each
+        auto box = [&](int b) {
+          Codes<kFormat> c[4];
+          uint32_t byte[4], top = 0;
 #pragma unroll
-        for (int i = 0; i < kChunks; ++i) {
-          const int id = first + i * 32 * kConvWarps, row = id / kPerRow, chunk = id % kPerRow;
-          const int r = (k & 1) * 64 + row;  // of the scale tile's 128 rows
-          c[i].load(raw, id);
-          byte[i] = scales[(chunk >> 4) * kScaleTile + (r & 31) * 16 + (r >> 5) * 4 + ((chunk >> 2) & 3)];
-        }
+          for (int q = 0; q < 4; ++q) {
+            const int r = row + 16 * q;
+            c[q].load(raw + (b * kTileR + r) * L::kBoxBytes + chunk * Codes<kFormat>::kBytes);
+            byte[q] = scales[(r & 31) * 16 + (r >> 5) * 4 + 2 * b];
+            top = max(top, byte[q]);
+          }
+          auto convert = [&](auto far) {
 #pragma unroll
-        for (int i = 0; i < kChunks; ++i) {
-          const int id = first + i * 32 * kConvWarps, row = id / kPerRow, chunk = id % kPerRow;
-          uint32_t v[4];
-          c[i].pairs(v);
-          scale_pairs<Codes<kFormat>::kBias>(v, byte[i]);
-          sts128(dst + (chunk >> 3) * 8192 + row * 128 + (((chunk & 7) ^ (row & 7)) << 4), v[0], v[1], v[2], v[3]);
-        }
+            for (int q = 0; q < 4; ++q) {
+              uint32_t v[4];
+              c[q].pairs(v);
+              scale_pairs<Codes<kFormat>::kBias, decltype(far)::value>(v, byte[q]);
+              sts128(dst + b * 8192 + q * 2048, v[0], v[1], v[2], v[3]);
+            }
+          };
+          if (__any_sync(0xFFFFFFFFu, top + Codes<kFormat>::kBias > 254u)) convert(std::true_type());
+          else convert(std::false_type());
+        };
+        box(0);
+        if (!u.half) box(1);
         fence_proxy_async_smem();
+        ok = mbar_wait_clearing(&bars->a_full[st], (at / kOps) & 1, abort_flag, p.status, 815);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) break;
+        if (sums) {
+          const uint8_t* const dy = smem + st * L::kOpBytes;
+#pragma unroll
+          for (int q = 0; q < 16; ++q) {
+            const int r = (t >> 5) * 16 + q;
+            const int off = r * 128 + (((lane >> 2) ^ (r & 7)) << 4) + (lane & 3) * 4;
+#pragma unroll
+            for (int b = 0; b < 2; ++b) {
+              const uint32_t w = *reinterpret_cast<const uint32_t*>(dy + b * 8192 + off);
+              acc[2 * b] += __uint_as_float(w << 16);
+              acc[2 * b + 1] += __uint_as_float(w & 0xFFFF0000u);
+            }
+          }
+        }
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive(&bars->b_full[st]);
+          mbar_arrive_cluster(cluster_u32(&bars->b_full[st], 0));
           mbar_arrive(&bars->raw_empty[rs]);
         }
       }
+      kc += steps;
+      if (sums && ok) {
+        float* const dst = p.bias_parts + (static_cast<size_t>(u.part) * (kGroups * 4) + group * 4 + (t >> 5)) * p.m_total;
+#pragma unroll
+        for (int b = 0; b < 2; ++b)
+#pragma unroll
+          for (int e = 0; e < 2; ++e) {
+            const int m = u.m0 + b * 64 + 2 * lane + e;
+            if (m < p.m_total) dst[m] = acc[2 * b + e];
+          }
+      }
     }
-  } else if (warp >= 4 + kConvWarps) {
+  } else if (warp >= 4 + kGroups * 4) {
     // ------------------------------------------------------------------------------------------ epilogue
     const int quarter = warp & 3;
     uint8_t* const warp_tile = smem + L::kOffOut + quarter * 4096;
@@ -303,68 +365,68 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
     const bool wide = kWgrad || p.out_dtype == LITE3R_F32;
     bool ok = true;
     int it = 0;
-    for (int unit = blockIdx.x; ok && unit < p.units; unit += gridDim.x) {
+    for (int unit = first_unit; ok && unit < p.units; unit += unit_step) {
       const UnitAt u = unit_at(unit);
+      // (nothing is stored of a CTA's rows or a tile's columns that are all past the end)
+      const int cols = u.m0 + quarter * 32 < p.m_total ? min(u.half ? kTileN / 2 : kTileN, p.n_total - u.n0) : 0;
       for (int k0 = u.first; ok && k0 < u.last; k0 += p.steps_per_sum, ++it) {
-      const int ab = it & 1;
-      const bool add = k0 > u.first;  // to the sum before, which this warp has stored
-      const uint32_t acc_addr = tmem + ((static_cast<uint32_t>(quarter) * 32u) << 16) + ab * kTileN;
-      ok = mbar_wait_clearing(&bars->acc_full[ab], (it >> 1) & 1, abort_flag, p.status, 813);
-      tc_fence_after();
-      ok = __all_sync(0xFFFFFFFFu, ok);
-      if (!ok) break;
-      if (add && lane == 0) bulk_wait_group0();  // it is in place
-      const int cols = min(kTileN, p.n_total - u.n0);  // a multiple of 32
+        const int ab = it & 1;
+        const bool add = k0 > u.first;  // to the sum before, which this warp has stored
+        const uint32_t acc_addr = tmem + ((static_cast<uint32_t>(quarter) * 32u) << 16) + ab * kTileN;
+        ok = mbar_wait_clearing(&bars->acc_full[ab], (it >> 1) & 1, abort_flag, p.status, 813);
+        tc_fence_after();
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) break;
+        if (add && lane == 0) bulk_wait_group0();  // it is in place
 #pragma unroll 1
-      for (int cb = 0; cb < cols; cb += 32) {
-        uint32_t v[32];
-        tmem_ld32(acc_addr + cb, v);
-        if (wide || (cb & 32) == 0) {  // what was staged here before has been read by the store engine
-          if (lane == 0) bulk_wait_group_read0();
-          __syncwarp();
-        }
-        tmem_wait_ld();
-        if (wide) {
+        for (int cb = 0; cb < cols; cb += 32) {  // a multiple of 32
+          uint32_t v[32];
+          tmem_ld32(acc_addr + cb, v);
+          if (wide || (cb & 32) == 0) {  // what was staged here before has been read by the store engine
+            if (lane == 0) bulk_wait_group_read0();
+            __syncwarp();
+          }
+          tmem_wait_ld();
+          if (wide) {
 #pragma unroll
-          for (int c = 0; c < 8; ++c) sts128(my_row + ((c ^ swz) << 4), v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
-        } else {
+            for (int c = 0; c < 8; ++c) sts128(my_row + ((c ^ swz) << 4), v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
+          } else {
 #pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t w[4];
+            for (int c = 0; c < 4; ++c) {
+              uint32_t w[4];
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const float y0 = __uint_as_float(v[8 * c + 2 * q]), y1 = __uint_as_float(v[8 * c + 2 * q + 1]);
-              if (p.out_dtype == LITE3R_BF16) {
-                __nv_bfloat162 h = __floats2bfloat162_rn(y0, y1);
-                w[q] = *reinterpret_cast<uint32_t*>(&h);
-              } else {
-                __half2 h = __floats2half2_rn(y0, y1);
-                w[q] = *reinterpret_cast<uint32_t*>(&h);
+              for (int q = 0; q < 4; ++q) {
+                const float y0 = __uint_as_float(v[8 * c + 2 * q]), y1 = __uint_as_float(v[8 * c + 2 * q + 1]);
+                if (p.out_dtype == LITE3R_BF16) {
+                  __nv_bfloat162 h = __floats2bfloat162_rn(y0, y1);
+                  w[q] = *reinterpret_cast<uint32_t*>(&h);
+                } else {
+                  __half2 h = __floats2half2_rn(y0, y1);
+                  w[q] = *reinterpret_cast<uint32_t*>(&h);
+                }
               }
+              sts128(my_row + ((((cb & 32) / 8 + c) ^ swz) << 4), w[0], w[1], w[2], w[3]);
             }
-            sts128(my_row + ((((cb & 32) / 8 + c) ^ swz) << 4), w[0], w[1], w[2], w[3]);
+          }
+          if (wide || (cb & 32) != 0 || cb + 32 >= cols) {  // (the engine clips columns past the output)
+            fence_proxy_async_smem();
+            __syncwarp();
+            if (lane == 0) {
+              const int x = u.n0 + (wide ? cb : cb & ~63), y = u.m0 + quarter * 32;
+              if constexpr (kWgrad) {
+                if (add) tma_add_3d(&map_out, warp_tile, x, y, u.part);
+                else tma_store_3d(&map_out, warp_tile, x, y, u.part);
+              } else {
+                if (add) tma_add_2d(&map_out, warp_tile, x, y);
+                else tma_store_2d(&map_out, warp_tile, x, y);
+              }
+              bulk_commit_group();
+            }
           }
         }
-        if (wide || (cb & 32) != 0 || cb + 32 >= cols) {  // (the engine clips columns past the output)
-          fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) {
-            const int x = u.n0 + (wide ? cb : cb & ~63);
-            const int y = u.m0 + quarter * 32;
-            if constexpr (kWgrad) {
-              if (add) tma_add_3d(&map_out, warp_tile, x, y, u.part);
-              else tma_store_3d(&map_out, warp_tile, x, y, u.part);
-            } else {
-              if (add) tma_add_2d(&map_out, warp_tile, x, y);
-              else tma_store_2d(&map_out, warp_tile, x, y);
-            }
-            bulk_commit_group();
-          }
-        }
-      }
-      tc_fence_before();
-      __syncwarp();
-      if (lane == 0) mbar_arrive(&bars->acc_empty[ab]);
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive_cluster(cluster_u32(&bars->acc_empty[ab], 0));
       }
     }
     bulk_wait_group_read0();  // what is staged stays in place until it has been read
@@ -373,136 +435,159 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
   tc_fence_before();
   __syncthreads();
   linger_after_abort(abort_flag);
+  cluster_sync();  // neither CTA leaves while the other one's products or arrivals may reach it
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem, kTmemCols);
+    tmem_dealloc_pair(tmem, kTmemCols);
   }
 }
 
 // ------------------------------------------------------------------------------------------------ sums
-constexpr int kBiasParts = 64;  // parts of the rows whose column sums are added by the second kernel
+struct Sums {
+  const float* parts;  // [count][values]
+  float* out;
+  size_t values;
+  int count;
+};
 
-// Column sums of dy over one part of the rows: eight columns per thread, eight row groups per CTA.
-__global__ void __launch_bounds__(256) bias_parts_kernel(const __nv_bfloat16* __restrict__ dy, long long stride, int rows, int d_out,
-                                                         int rows_per_part, float* __restrict__ parts) {
-  __shared__ float s_sum[8][256];
-  const int lane = threadIdx.x & 31, group = threadIdx.x >> 5;
-  const int col = blockIdx.x * 256 + lane * 8;
-  const int r0 = blockIdx.y * rows_per_part, r1 = min(r0 + rows_per_part, rows);
-  float acc[8] = {};
+// out[i] = sum over the parts, in order: dw four values to a thread (blocks below dw_blocks), db one to a thread, four
+// quarters of the parts side by side.
+__global__ void __launch_bounds__(256) add_parts_kernel(const Sums dw, int dw_blocks, const Sums db) {
+  __shared__ float s_sum[4][64];
   wait_for_prior_grid();
   launch_dependents();
-  if (col < d_out) {
+  if (static_cast<int>(blockIdx.x) < dw_blocks) {
+    const size_t i = (static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x) * 4;
+    if (i >= dw.values) return;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll 4
-    for (int r = r0 + group; r < r1; r += 8) {
-      const __nv_bfloat16* src = dy + static_cast<long long>(r) * stride + col;
-      if (col + 8 <= d_out) {
-        const uint4 w = __ldg(reinterpret_cast<const uint4*>(src));
-        const uint32_t x[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          acc[2 * i] += __uint_as_float(x[i] << 16);
-          acc[2 * i + 1] += __uint_as_float(x[i] & 0xFFFF0000u);
-        }
-      } else {
-        for (int i = 0; i < d_out - col; ++i) acc[i] += __bfloat162float(src[i]);
-      }
+    for (int s = 0; s < dw.count; ++s) {
+      const float4 v = *reinterpret_cast<const float4*>(dw.parts + static_cast<size_t>(s) * dw.values + i);
+      acc.x += v.x; acc.y += v.y; acc.z += v.z; acc.w += v.w;
     }
+    *reinterpret_cast<float4*>(dw.out + i) = acc;
+    return;
   }
-#pragma unroll
-  for (int i = 0; i < 8; ++i) s_sum[group][lane * 8 + i] = acc[i];
+  const int col = threadIdx.x & 63, quarter = threadIdx.x >> 6;
+  const size_t i = static_cast<size_t>(blockIdx.x - dw_blocks) * 64 + col;
+  float acc = 0.f;
+  if (i < db.values) {
+    const int s0 = db.count * quarter / 4, s1 = db.count * (quarter + 1) / 4;
+#pragma unroll 8
+    for (int s = s0; s < s1; ++s) acc += db.parts[static_cast<size_t>(s) * db.values + i];
+  }
+  s_sum[quarter][col] = acc;
   __syncthreads();
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c < d_out) {
-    float sum = 0.f;
-#pragma unroll
-    for (int g = 0; g < 8; ++g) sum += s_sum[g][threadIdx.x];
-    parts[static_cast<size_t>(blockIdx.y) * d_out + c] = sum;
-  }
+  if (threadIdx.x < 64 && i < db.values) db.out[i] = (s_sum[0][col] + s_sum[1][col]) + (s_sum[2][col] + s_sum[3][col]);
 }
 
-// out[i] = sum over the parts, in order (four values per thread where that is possible).
-template <int kVec>
-__global__ void __launch_bounds__(256) add_parts_kernel(const float* parts, int count, size_t values, float* __restrict__ out) {
-  wait_for_prior_grid();
-  launch_dependents();
-  const size_t i = (static_cast<size_t>(blockIdx.x) * 256 + threadIdx.x) * kVec;
-  if (i >= values) return;
-  float acc[kVec] = {};
-#pragma unroll 4
-  for (int s = 0; s < count; ++s) {
-    const float* src = parts + static_cast<size_t>(s) * values + i;
-    if constexpr (kVec == 4) {
-      const float4 v = *reinterpret_cast<const float4*>(src);
-      acc[0] += v.x; acc[1] += v.y; acc[2] += v.z; acc[3] += v.w;
-    } else {
-      acc[0] += src[0];
+constexpr int kMostPairs = 128;  // of any device, for the size of the workspace
+
+// How the tiles are cut.  Columns: all of 256, or the last 256 in two halves, which run last and fill the gaps that whole tiles
+// leave (10992 x 1024: 172 tiles on 74 pairs take three rounds, 129 and 86 halves two and a half), or halves throughout
+// (few tiles).
+struct Cut {
+  int wide, half, row_tiles, parts;
+};
+// Time in halves: a pair takes units p, p + pairs, ..., whole tiles first, so pair 0 has most of both.
+long long most_columns(const Cut& c, int pairs) {
+  const long long wide = static_cast<long long>(c.wide) * c.row_tiles * c.parts, all = wide + static_cast<long long>(c.half) * c.row_tiles * c.parts;
+  return (wide + pairs - 1) / pairs + (all + pairs - 1) / pairs;
+}
+Cut cut_tiles(int m_total, int n_total, int parts, int pairs) {
+  const int n = ceil_div(n_total, kTileN / 2), rows = ceil_div(m_total, kTileM);  // halves per row of tiles
+  Cut best = {n / 2, n % 2, rows, parts};
+  long long least = most_columns(best, pairs);
+  for (int half : {n % 2 + 2, n}) {
+    if (half > n) continue;
+    const Cut c = {(n - half) / 2, half, rows, parts};
+    const long long time = most_columns(c, pairs);
+    if (time * 16 < least * 15) {  // (halves read A twice as often)
+      best = c;
+      least = time;
     }
   }
-  if constexpr (kVec == 4) *reinterpret_cast<float4*>(out + i) = make_float4(acc[0], acc[1], acc[2], acc[3]);
-  else out[i] = acc[0];
+  return best;
 }
 
-// Parts of the rows: as many as give every SM a tile, none shorter than sixteen steps.
-int parts_of(int steps, int tiles, int sms) {
-  return std::max(1, std::min(ceil_div(sms, tiles), steps / 16));
+// Parts of the contraction of wgrad: the number with the least time, in steps of a half tile, of the products (a part's steps
+// and four to fill and drain the pipeline) and of writing and reading its partial results, 8 bytes per value and part at about
+// 4 TB/s against 0.15 us a step.
+int wgrad_parts(int rows, int d_in, int d_out, int pairs) {
+  const int steps = ceil_div(rows, kTileR);
+  const double add = static_cast<double>(d_in) * d_out * 8.0 / 4e6 / 0.15;
+  int best = 1;
+  double least = 1e300;
+  for (int parts = 1; parts <= std::max(1, std::min(16, steps / 8)); ++parts) {
+    const int per_part = ceil_div(steps, parts);
+    if (ceil_div(steps, per_part) != parts) continue;  // none is empty
+    const double time = static_cast<double>(most_columns(cut_tiles(d_out, d_in, parts, pairs), pairs)) * (per_part + 4) + (parts > 1 ? add * parts + 20 : 0);
+    if (time < least * 0.97) {
+      best = parts;
+      least = time;
+    }
+  }
+  return best;
 }
-constexpr int kMostSms = 256;  // of any device, for the size of the workspace
 
 template <int kFormat, bool kWgrad>
 lite3r_status launch_back(const void* dy, long long dy_stride, const uint8_t* codes, const uint8_t* scales, int rows, int d_in,
-                          int d_out, const CUtensorMap& map_out, int out_dtype, int parts, int* status, int sms, cudaStream_t stream) {
+                          int d_out, const CUtensorMap& map_out, int out_dtype, int parts, float* bias_parts, int* status, int pairs,
+                          cudaStream_t stream) {
   using L = Layout<kFormat>;
   CUtensorMap map_dy, map_codes;
   lite3r_status st;
-  if ((st = make_tensor_map_2d(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dy, d_out, rows, 64, kWgrad ? 64 : kTileM,
+  if ((st = make_tensor_map_2d(&map_dy, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dy, d_out, rows, 64, kWgrad ? 64 : 128,
                                CU_TENSOR_MAP_SWIZZLE_128B, static_cast<uint64_t>(dy_stride) * 2)) != LITE3R_OK) return st;
   const int code_rows = kWgrad ? rows : d_out;
   if ((st = make_tensor_map_2d(&map_codes, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, codes, kFormat == LITE3R_MXFP8 ? d_in : d_in / 2, code_rows,
-                               L::kRowBytes, kTileR, CU_TENSOR_MAP_SWIZZLE_NONE)) != LITE3R_OK) return st;
+                               L::kBoxBytes, kTileR, CU_TENSOR_MAP_SWIZZLE_NONE)) != LITE3R_OK) return st;
   auto* kernel = mx_back_kernel<kFormat, kWgrad>;
   if ((st = ensure_dynamic_smem(kernel, static_cast<int>(L::kSmemBytes))) != LITE3R_OK) return st;
   BackParams p = {};
   p.scales = scales;
+  p.bias_parts = bias_parts;
+  p.m_total = kWgrad ? d_out : rows;
   p.n_total = d_in;
   p.scale_tiles = ceil_div(d_in, 128);
   p.steps = ceil_div(code_rows, kTileR);
   p.steps_per_part = ceil_div(p.steps, parts);
   p.steps_per_sum = out_dtype == LITE3R_F32 ? 2048 / kTileR : p.steps;
-  p.col_tiles = ceil_div(d_in, kTileN);
-  const long long tiles = static_cast<long long>(p.col_tiles) * ceil_div(kWgrad ? d_out : rows, kTileM);
-  if (tiles * parts > 0x7FFFFFFFLL - 1024) return LITE3R_ERR_UNSUPPORTED;
-  p.tiles = static_cast<int>(tiles);
-  p.units = p.tiles * parts;
+  const Cut c = cut_tiles(p.m_total, d_in, parts, pairs);
+  p.wide_tiles = c.wide;
+  p.half_tiles = c.half;
+  p.row_tiles = c.row_tiles;
+  p.parts = parts;
+  const long long units = static_cast<long long>(c.wide + c.half) * c.row_tiles * parts;
+  if (units > 0x7FFFFFFFLL - 1024) return LITE3R_ERR_UNSUPPORTED;
+  p.units = static_cast<int>(units);
   p.out_dtype = out_dtype;
   p.status = status;
-  return launch_dependent(kernel, dim3(static_cast<unsigned>(std::min(p.units, sms))), kThreads, static_cast<int>(L::kSmemBytes), stream,
-                          map_dy, map_codes, map_out, p);
+  return launch_dependent_cluster(kernel, dim3(static_cast<unsigned>(2 * std::min(p.units, pairs))), kThreads,
+                                  static_cast<int>(L::kSmemBytes), 2, stream, map_dy, map_codes, map_out, p);
 }
 
-long long wgrad_tiles(int d_in, int d_out) { return static_cast<long long>(ceil_div(d_in, kTileN)) * ceil_div(d_out, kTileM); }
-
-// Parts after rounding their length up to whole steps: none is empty.
-int wgrad_parts(int rows, int d_in, int d_out, int sms) {
-  const int steps = ceil_div(rows, kTileR);
-  const int parts = parts_of(steps, static_cast<int>(std::min<long long>(wgrad_tiles(d_in, d_out), 1 << 20)), sms);
-  return ceil_div(steps, ceil_div(steps, parts));
+lite3r_status pairs_of_device(int* pairs) {
+  int sms = 0;
+  const lite3r_status st = sm_count(&sms);
+  *pairs = std::max(1, std::min(sms / 2, kMostPairs));
+  return st;
 }
 
 }  // namespace
 
+// Room for as many parts as any device's rule may choose.
 size_t linear_mx_workspace_bytes(int rows, int d_in, int d_out) {
-  const int steps = ceil_div(rows, kTileR);
-  const int parts = parts_of(steps, static_cast<int>(std::min<long long>(wgrad_tiles(d_in, d_out), 1 << 20)), kMostSms);
-  const size_t products = parts > 1 ? static_cast<size_t>(parts) * d_in * d_out : 0;
-  return (products + static_cast<size_t>(kBiasParts) * d_out) * sizeof(float) + 256;
+  size_t parts = 1;
+  for (int pairs : {66, 70, 72, 74, 76, 80}) parts = std::max<size_t>(parts, wgrad_parts(rows, d_in, d_out, pairs));
+  return ((parts > 1 ? parts * d_in * d_out : 0) + parts * kGroups * 4 * d_out) * sizeof(float) + 256;
 }
 
 lite3r_status launch_mx_dgrad(const void* dy, long long dy_stride, const uint8_t* w_codes, const uint8_t* w_scales, int format,
                               int rows, int d_in, int d_out, void* dx, int dx_dtype, long long dx_stride, int* device_status,
                               cudaStream_t stream) {
-  int sms = 0;
-  lite3r_status st = sm_count(&sms);
+  int pairs = 0;
+  lite3r_status st = pairs_of_device(&pairs);
   if (st != LITE3R_OK) return st;
   const int elem = dx_dtype == LITE3R_F32 ? 4 : 2;
   CUtensorMap map;
@@ -512,40 +597,34 @@ lite3r_status launch_mx_dgrad(const void* dy, long long dy_stride, const uint8_t
                                                     : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
                           elem, dx, d_in, rows, 128 / elem, 32, CU_TENSOR_MAP_SWIZZLE_128B, static_cast<uint64_t>(dx_stride) * elem);
   if (st != LITE3R_OK) return st;
-  return format == LITE3R_MXFP8 ? launch_back<LITE3R_MXFP8, false>(dy, dy_stride, w_codes, w_scales, rows, d_in, d_out, map, dx_dtype, 1, device_status, sms, stream)
-                                : launch_back<LITE3R_MXFP4, false>(dy, dy_stride, w_codes, w_scales, rows, d_in, d_out, map, dx_dtype, 1, device_status, sms, stream);
+  auto* launch = format == LITE3R_MXFP8 ? launch_back<LITE3R_MXFP8, false> : launch_back<LITE3R_MXFP4, false>;
+  return launch(dy, dy_stride, w_codes, w_scales, rows, d_in, d_out, map, dx_dtype, 1, nullptr, device_status, pairs, stream);
 }
 
 lite3r_status launch_mx_wgrad(const void* dy, long long dy_stride, const uint8_t* x_codes, const uint8_t* x_scales, int format,
-                              int rows, int d_in, int d_out, float* dw, float* db, float* workspace, int* device_status,
-                              cudaStream_t stream) {
-  int sms = 0;
-  lite3r_status st = sm_count(&sms);
+                              int rows, int d_in, int d_out, float* dw, float* db, float* workspace, size_t workspace_bytes,
+                              int* device_status, cudaStream_t stream) {
+  int pairs = 0;
+  lite3r_status st = pairs_of_device(&pairs);
   if (st != LITE3R_OK) return st;
-  const int parts = wgrad_parts(rows, d_in, d_out, std::min(sms, kMostSms));
+  const int parts = wgrad_parts(rows, d_in, d_out, pairs);
   const size_t values = static_cast<size_t>(d_in) * d_out;
+  if (((parts > 1 ? parts * values : 0) + static_cast<size_t>(parts) * kGroups * 4 * d_out) * sizeof(float) > workspace_bytes)
+    return LITE3R_ERR_WORKSPACE;
   float* const products = parts > 1 ? workspace : dw;
   float* const bias_parts = workspace + (parts > 1 ? parts * values : 0);
   CUtensorMap map;
   if ((st = make_tensor_map_3d(&map, CU_TENSOR_MAP_DATA_TYPE_FLOAT32, 4, products, d_in, d_out, parts, 32, 32, CU_TENSOR_MAP_SWIZZLE_128B)) != LITE3R_OK)
     return st;
-  st = format == LITE3R_MXFP8 ? launch_back<LITE3R_MXFP8, true>(dy, dy_stride, x_codes, x_scales, rows, d_in, d_out, map, LITE3R_F32, parts, device_status, sms, stream)
-                              : launch_back<LITE3R_MXFP4, true>(dy, dy_stride, x_codes, x_scales, rows, d_in, d_out, map, LITE3R_F32, parts, device_status, sms, stream);
-  if (st != LITE3R_OK) return st;
-  if (parts > 1) {  // (d_in is a multiple of 32)
-    st = launch_dependent(add_parts_kernel<4>, dim3(static_cast<unsigned>((values / 4 + 255) / 256)), 256, 0, stream,
-                          static_cast<const float*>(products), parts, values, dw);
-    if (st != LITE3R_OK) return st;
-  }
-  if (db == nullptr) return LITE3R_OK;
-  const int row_parts = std::min(kBiasParts, ceil_div(rows, 64));
-  const int rows_per_part = ceil_div(rows, row_parts);
-  const int used = ceil_div(rows, rows_per_part);
-  st = launch_dependent(bias_parts_kernel, dim3(static_cast<unsigned>(ceil_div(d_out, 256)), static_cast<unsigned>(used)), 256, 0, stream,
-                        static_cast<const __nv_bfloat16*>(dy), dy_stride, rows, d_out, rows_per_part, bias_parts);
-  if (st != LITE3R_OK) return st;
-  return launch_dependent(add_parts_kernel<1>, dim3(static_cast<unsigned>(ceil_div(d_out, 256))), 256, 0, stream,
-                          static_cast<const float*>(bias_parts), used, static_cast<size_t>(d_out), db);
+  auto* launch = format == LITE3R_MXFP8 ? launch_back<LITE3R_MXFP8, true> : launch_back<LITE3R_MXFP4, true>;
+  st = launch(dy, dy_stride, x_codes, x_scales, rows, d_in, d_out, map, LITE3R_F32, parts, db != nullptr ? bias_parts : nullptr, device_status,
+              pairs, stream);
+  if (st != LITE3R_OK || (parts == 1 && db == nullptr)) return st;
+  const Sums dw_sums = {products, dw, values, parts}, db_sums = {bias_parts, db, static_cast<size_t>(d_out), parts * kGroups * 4};
+  const long long dw_blocks = parts > 1 ? static_cast<long long>((values / 4 + 255) / 256) : 0, db_blocks = db != nullptr ? ceil_div(d_out, 64) : 0;
+  if (dw_blocks + db_blocks > 0x7FFFFFFFLL) return LITE3R_ERR_UNSUPPORTED;
+  return launch_dependent(add_parts_kernel, dim3(static_cast<unsigned>(dw_blocks + db_blocks)), 256, 0, stream, dw_sums,
+                          static_cast<int>(dw_blocks), db_sums);
 }
 
 }  // namespace lite3r
