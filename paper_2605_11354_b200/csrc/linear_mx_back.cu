@@ -340,7 +340,7 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
         }
         __syncwarp();
         if (lane == 0) {
-          mbar_arrive_cluster(cluster_u32(&bars->b_full[st], 0));
+          mbar_arrive_cluster_own(cluster_u32(&bars->b_full[st], 0));
           mbar_arrive(&bars->raw_empty[rs]);
         }
       }

@@ -385,6 +385,12 @@ __device__ __forceinline__ uint32_t cluster_u32(const void* p, uint32_t rank) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
+// The same after writes to this CTA's own shared memory that a product of the pair will read from there: their order need only
+// hold where they are, in this CTA (a release at cluster scope waits until everything is performed for the whole GPU: 1800
+// cycles in the converting warps of the backward GEMM).
+__device__ __forceinline__ void mbar_arrive_cluster_own(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
 // 2-D tile load into this CTA's shared memory, counted in bytes on a barrier of either CTA of the pair.
 __device__ __forceinline__ void tma_load_2d_pair(void* smem_dst, const CUtensorMap* map, uint32_t cluster_bar, int x, int y) {
   asm volatile(
