@@ -11,8 +11,8 @@
 // the pair's first CTA issues the products into one of two accumulators, four warps are the epilogue.
 // The sixteen warps work in four groups, each on every fourth step: a step's chain of load, arithmetic, store and proxy fence
 // takes longer than its products (1900 cycles of a step with all warps on the same one, 512 of products), four chains side by
-// side do not.  Each CTA converts half of B for the pair, about 30 instructions per eight values.  The warps that convert the
-// first column tile's steps of wgrad also add up the columns of dy for db while its tile lies in shared memory.
+// side do not.  Each CTA converts half of B for the pair.  For db the groups also add up the columns of dy while its tile lies
+// in shared memory, the first four column tiles by turns.
 //
 // The tensor cores' running sum is cut off, not rounded, at fp32: it drifts towards zero by about 4e-9 of the result per
 // product of 16 steps (10992 rows in one sum: dW off by 2.6e-6).  Results in fp32 are therefore summed over 2048 steps at a time
@@ -61,12 +61,13 @@ struct Bars {
 
 struct BackParams {
   const uint8_t* scales;
-  float* bias_parts;          // wgrad: [parts][groups][4 warps][m_total], or null
+  float* bias_parts;          // wgrad: [parts x groups][bias_cols][4 warps][m_total], or null
   int m_total, n_total;       // rows and columns of the result
   int scale_tiles;            // along n
   int steps, steps_per_part;  // of 64 along the contraction, in all and of one part of it
   int steps_per_sum;          // of one running sum in tensor memory
   int wide_tiles, half_tiles; // columns of a row of tiles: those of 256 first, then those of 128
+  int bias_cols;              // column tiles that share the sums of dy
   int row_tiles, parts, units;
   int out_dtype;
   int* status;
@@ -77,37 +78,38 @@ __device__ __forceinline__ uint32_t mul_bf16x2(uint32_t a, uint32_t b) {
   return *reinterpret_cast<const uint32_t*>(&r);
 }
 
-// Eight codes of a row to bf16 pairs.  A code's sign goes to bit 15, its exponent behind bf16's bias and its mantissa on top of
-// seven bits: that is the value times 2^-kBias (denormals included), which the block's factor 2^(byte - 127 + kBias) undoes.
+// Sixteen codes of a row to bf16 pairs.  A code's sign goes to bit 15, its exponent behind bf16's bias and its mantissa on top
+// of seven bits: that is the value times 2^-kBias (denormals included), which the block's factor 2^(byte - 127 + kBias) undoes.
 template <int kFormat>
 struct Codes;
 template <>
 struct Codes<LITE3R_MXFP8> {
-  static constexpr int kBias = 120;
-  uint2 w;
-  __device__ __forceinline__ void load(const uint8_t* at) { w = *reinterpret_cast<const uint2*>(at); }
-  static constexpr int kBytes = 8;
+  static constexpr int kBias = 120, kBytes = 16;
+  uint4 w;
+  __device__ __forceinline__ void load(uint32_t at) { w = lds128(at); }
   static __device__ __forceinline__ uint32_t spread(uint32_t pair) { return ((pair >> 4) & 0x07F007F0u) | (pair & 0x80008000u); }
-  __device__ __forceinline__ void pairs(uint32_t out[4]) const {
-    out[0] = spread(__byte_perm(w.x, 0u, 0x1404));
-    out[1] = spread(__byte_perm(w.x, 0u, 0x3424));
-    out[2] = spread(__byte_perm(w.y, 0u, 0x1404));
-    out[3] = spread(__byte_perm(w.y, 0u, 0x3424));
+  __device__ __forceinline__ void pairs(int half, uint32_t out[4]) const {
+    const uint32_t x = half == 0 ? w.x : w.z, y = half == 0 ? w.y : w.w;
+    out[0] = spread(__byte_perm(x, 0u, 0x1404));
+    out[1] = spread(__byte_perm(x, 0u, 0x3424));
+    out[2] = spread(__byte_perm(y, 0u, 0x1404));
+    out[3] = spread(__byte_perm(y, 0u, 0x3424));
   }
 };
 template <>
 struct Codes<LITE3R_MXFP4> {
-  static constexpr int kBias = 126;
-  uint32_t w;
-  __device__ __forceinline__ void load(const uint8_t* at) { w = *reinterpret_cast<const uint32_t*>(at); }
-  static constexpr int kBytes = 4;
+  static constexpr int kBias = 126, kBytes = 8;
+  uint32_t w[2];
+  __device__ __forceinline__ void load(uint32_t at) {
+    asm volatile("ld.shared.v2.u32 {%0, %1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(at) : "memory");
+  }
   static __device__ __forceinline__ uint32_t spread(uint32_t pair) { return ((pair >> 6) & 0x01C001C0u) | (pair & 0x80008000u); }
-  __device__ __forceinline__ void pairs(uint32_t out[4]) const {
-    const uint32_t even = w << 4;  // the even columns' codes in the bytes' upper halves, as the odd ones' are in w
-    out[0] = spread(__byte_perm(even, w, 0x4004));  // (what else is in these bytes the masks take away)
-    out[1] = spread(__byte_perm(even, w, 0x5111));
-    out[2] = spread(__byte_perm(even, w, 0x6222));
-    out[3] = spread(__byte_perm(even, w, 0x7333));
+  __device__ __forceinline__ void pairs(int half, uint32_t out[4]) const {
+    const uint32_t odd = w[half], even = odd << 4;  // the even columns' codes in the bytes' upper halves, as the odd ones' are
+    out[0] = spread(__byte_perm(even, odd, 0x4004));  // (what else is in these bytes the masks take away)
+    out[1] = spread(__byte_perm(even, odd, 0x5111));
+    out[2] = spread(__byte_perm(even, odd, 0x6222));
+    out[3] = spread(__byte_perm(even, odd, 0x7333));
   }
 };
 
@@ -176,6 +178,7 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
   const int wide_units = p.wide_tiles * p.row_tiles * p.parts;
   struct UnitAt {
     int m0, n0, part, first, last;  // this CTA's rows, the pair's columns, steps [first, last) of the contraction
+    int col;                        // column tile
     bool half;
   };
   auto unit_at = [&](int unit) {
@@ -187,6 +190,7 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
     u.part = kWgrad ? unit / per_part : 0;
     const int tile = unit - u.part * per_part, row_tile = tile / cols, col = tile - row_tile * cols;
     u.m0 = row_tile * kTileM + rank * 128;
+    u.col = u.half ? p.wide_tiles + col : col;
     u.n0 = u.half ? p.wide_tiles * kTileN + col * (kTileN / 2) : col * kTileN;
     u.first = u.part * p.steps_per_part;
     u.last = min(u.first + p.steps_per_part, p.steps);
@@ -275,56 +279,59 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
   } else if (warp >= 4 && warp < 4 + kGroups * 4) {
     // ------------------------------------------------------------------------------------------ codes to bf16
     const int group = (warp - 4) >> 2, t = threadIdx.x & (kGroupThreads - 1);
-    const int row = t >> 3, chunk = t & 7;  // of sixteen rows and eight chunks of eight columns at a time
+    const int row = t >> 2, chunk = t & 3;  // of 32 rows and four chunks of sixteen columns at a time
+    const uint32_t my_raw = smem_u32(smem) + L::kOffRaw + row * L::kBoxBytes + chunk * Codes<kFormat>::kBytes;
+    const uint32_t my_scales = smem_u32(smem) + L::kOffRaw + L::kOffScales + row * 16;
+    const uint32_t my_b = smem_u32(smem) + L::kOffB + row * 128 + (((2 * chunk) ^ (row & 7)) << 4);  // and the next chunk's 16 bytes: ^ 16
     bool ok = true;
     int kc = 0;
     for (int unit = first_unit; ok && unit < p.units; unit += unit_step) {
       const UnitAt u = unit_at(unit);
-      const int block = (u.half ? 2 * rank : 0) + (chunk >> 2);  // of the scale tile's four, for the first box
-      const bool sums = kWgrad && p.bias_parts != nullptr && u.n0 == 0 && u.m0 < p.m_total;
+      const int shift = 8 * ((u.half ? 2 * rank : 0) + (chunk >> 1));  // of the scale tile's four blocks, for the first box
+      const bool sums = kWgrad && p.bias_parts != nullptr && u.col < p.bias_cols && u.m0 < p.m_total;
       float acc[4] = {};  // columns 2 lane, 2 lane + 1 of the two boxes of dy, over this warp's rows
       const int steps = u.last - u.first;
-      // the first step of the unit that is this group's
-      for (int i = (group - kc % kGroups + kGroups) % kGroups; ok && i < steps; i += kGroups) {
+      const int mine = (group - kc % kGroups + kGroups) % kGroups;  // the first step of the unit that is this group's
+      for (int i = mine; ok && i < steps; i += kGroups) {
         const int at = kc + i, k = u.first + i;
         const int rs = at % kRaw, st = at % kOps;
         ok = mbar_wait_clearing(&bars->raw_full[rs], (at / kRaw) & 1, abort_flag, p.status, 817);
         if (ok && at >= kOps) ok = mbar_wait_clearing(&bars->op_empty[st], ((at - kOps) / kOps) & 1, abort_flag, p.status, 818);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
-        const uint8_t* const raw = smem + L::kOffRaw + rs * L::kRawBytes;
-        const uint8_t* const scales = raw + L::kOffScales + ((k & 1) * 2) * 4 + block;
-        const uint32_t dst = smem_u32(smem) + st * L::kOpBytes + L::kOffB + row * 128 + ((chunk ^ (row & 7)) << 4);
-        // two boxes (a half tile: one) of 64 columns, four times sixteen rows each
-        auto box = [&](int b) {
-          Codes<kFormat> c[4];
-          uint32_t byte[4], top = 0;
+        const uint32_t raw = my_raw + rs * L::kRawBytes, dst = my_b + st * L::kOpBytes;
+        Codes<kFormat> c[4];  // [box][32 rows]
+        uint32_t byte[4], top = 0;
+#pragma unroll
+        for (int q = 0; q < 2; ++q) {
+          uint32_t word;  // of row (k & 1) * 64 + row + 32 q of the scale tile
+          asm volatile("ld.shared.u32 %0, [%1];" : "=r"(word) : "r"(my_scales + rs * L::kRawBytes + ((k & 1) * 2 + q) * 4) : "memory");
+          byte[q] = (word >> shift) & 0xFFu;
+          byte[2 + q] = u.half ? byte[q] : (word >> (shift + 16)) & 0xFFu;
+          top = max(top, max(byte[q], byte[2 + q]));
+          c[q].load(raw + q * (32 * L::kBoxBytes));
+          if (!u.half) c[2 + q].load(raw + (kTileR + 32 * q) * L::kBoxBytes);
+        }
+        auto convert = [&](auto far) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
-            const int r = row + 16 * q;
-            c[q].load(raw + (b * kTileR + r) * L::kBoxBytes + chunk * Codes<kFormat>::kBytes);
-            byte[q] = scales[(r & 31) * 16 + (r >> 5) * 4 + 2 * b];
-            top = max(top, byte[q]);
-          }
-          auto convert = [&](auto far) {
+            if (q >= 2 && u.half) break;
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
+            for (int h = 0; h < 2; ++h) {
               uint32_t v[4];
-              c[q].pairs(v);
+              c[q].pairs(h, v);
               scale_pairs<Codes<kFormat>::kBias, decltype(far)::value>(v, byte[q]);
-              sts128(dst + b * 8192 + q * 2048, v[0], v[1], v[2], v[3]);
+              sts128((dst ^ (h << 4)) + (q >> 1) * 8192 + (q & 1) * 4096, v[0], v[1], v[2], v[3]);
             }
-          };
-          if (__any_sync(0xFFFFFFFFu, top + Codes<kFormat>::kBias > 254u)) convert(std::true_type());
-          else convert(std::false_type());
+          }
         };
-        box(0);
-        if (!u.half) box(1);
+        if (__any_sync(0xFFFFFFFFu, top + Codes<kFormat>::kBias > 254u)) convert(std::true_type());
+        else convert(std::false_type());
         fence_proxy_async_smem();
         ok = mbar_wait_clearing(&bars->a_full[st], (at / kOps) & 1, abort_flag, p.status, 815);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
-        if (sums) {
+        if (sums && k % p.bias_cols == u.col) {
           const uint8_t* const dy = smem + st * L::kOpBytes;
 #pragma unroll
           for (int q = 0; q < 16; ++q) {
@@ -345,15 +352,13 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
         }
       }
       kc += steps;
-      if (sums && ok) {
-        float* const dst = p.bias_parts + (static_cast<size_t>(u.part) * (kGroups * 4) + group * 4 + (t >> 5)) * p.m_total;
+      if (sums && ok && mine < steps) {
+        float* const dst = p.bias_parts + (static_cast<size_t>((u.part * kGroups + mine) * p.bias_cols + u.col) * 4 + (t >> 5)) * p.m_total;
 #pragma unroll
-        for (int b = 0; b < 2; ++b)
-#pragma unroll
-          for (int e = 0; e < 2; ++e) {
-            const int m = u.m0 + b * 64 + 2 * lane + e;
-            if (m < p.m_total) dst[m] = acc[2 * b + e];
-          }
+        for (int e = 0; e < 4; ++e) {
+          const int m = u.m0 + (e >> 1) * 64 + 2 * lane + (e & 1);
+          if (m < p.m_total) dst[m] = acc[e];
+        }
       }
     }
   } else if (warp >= 4 + kGroups * 4) {
@@ -481,6 +486,7 @@ __global__ void __launch_bounds__(256) add_parts_kernel(const Sums dw, int dw_bl
   if (threadIdx.x < 64 && i < db.values) db.out[i] = (s_sum[0][col] + s_sum[1][col]) + (s_sum[2][col] + s_sum[3][col]);
 }
 
+constexpr int kBiasCols = 4;
 constexpr int kMostPairs = 128;  // of any device, for the size of the workspace
 
 // How the tiles are cut.  Columns: all of 256, or the last 256 in two halves, which run last and fill the gaps that whole tiles
@@ -556,6 +562,7 @@ lite3r_status launch_back(const void* dy, long long dy_stride, const uint8_t* co
   const Cut c = cut_tiles(p.m_total, d_in, parts, pairs);
   p.wide_tiles = c.wide;
   p.half_tiles = c.half;
+  p.bias_cols = std::min(kBiasCols, c.wide + c.half);
   p.row_tiles = c.row_tiles;
   p.parts = parts;
   const long long units = static_cast<long long>(c.wide + c.half) * c.row_tiles * parts;
@@ -580,7 +587,7 @@ lite3r_status pairs_of_device(int* pairs) {
 size_t linear_mx_workspace_bytes(int rows, int d_in, int d_out) {
   size_t parts = 1;
   for (int pairs : {66, 70, 72, 74, 76, 80}) parts = std::max<size_t>(parts, wgrad_parts(rows, d_in, d_out, pairs));
-  return ((parts > 1 ? parts * d_in * d_out : 0) + parts * kGroups * 4 * d_out) * sizeof(float) + 256;
+  return ((parts > 1 ? parts * d_in * d_out : 0) + parts * kGroups * kBiasCols * 4 * d_out) * sizeof(float) + 256;
 }
 
 lite3r_status launch_mx_dgrad(const void* dy, long long dy_stride, const uint8_t* w_codes, const uint8_t* w_scales, int format,
@@ -609,7 +616,7 @@ lite3r_status launch_mx_wgrad(const void* dy, long long dy_stride, const uint8_t
   if (st != LITE3R_OK) return st;
   const int parts = wgrad_parts(rows, d_in, d_out, pairs);
   const size_t values = static_cast<size_t>(d_in) * d_out;
-  if (((parts > 1 ? parts * values : 0) + static_cast<size_t>(parts) * kGroups * 4 * d_out) * sizeof(float) > workspace_bytes)
+  if (((parts > 1 ? parts * values : 0) + static_cast<size_t>(parts) * kGroups * kBiasCols * 4 * d_out) * sizeof(float) > workspace_bytes)
     return LITE3R_ERR_WORKSPACE;
   float* const products = parts > 1 ? workspace : dw;
   float* const bias_parts = workspace + (parts > 1 ? parts * values : 0);
@@ -620,7 +627,11 @@ lite3r_status launch_mx_wgrad(const void* dy, long long dy_stride, const uint8_t
   st = launch(dy, dy_stride, x_codes, x_scales, rows, d_in, d_out, map, LITE3R_F32, parts, db != nullptr ? bias_parts : nullptr, device_status,
               pairs, stream);
   if (st != LITE3R_OK || (parts == 1 && db == nullptr)) return st;
-  const Sums dw_sums = {products, dw, values, parts}, db_sums = {bias_parts, db, static_cast<size_t>(d_out), parts * kGroups * 4};
+  // a part of fewer than four steps (the last, or the only one) has no sums of the groups without a step
+  const int steps = ceil_div(rows, kTileR), last = steps - (parts - 1) * ceil_div(steps, parts);
+  const Cut c = cut_tiles(d_out, d_in, parts, pairs);
+  const int bias_count = ((parts - 1) * kGroups + std::min(kGroups, last)) * std::min(kBiasCols, c.wide + c.half) * 4;
+  const Sums dw_sums = {products, dw, values, parts}, db_sums = {bias_parts, db, static_cast<size_t>(d_out), bias_count};
   const long long dw_blocks = parts > 1 ? static_cast<long long>((values / 4 + 255) / 256) : 0, db_blocks = db != nullptr ? ceil_div(d_out, 64) : 0;
   if (dw_blocks + db_blocks > 0x7FFFFFFFLL) return LITE3R_ERR_UNSUPPORTED;
   return launch_dependent(add_parts_kernel, dim3(static_cast<unsigned>(dw_blocks + db_blocks)), 256, 0, stream, dw_sums,
