@@ -2,10 +2,13 @@
 // scale per 32 elements of K, fp32 accumulation in TMEM).
 // A product of two e2m1 values is a multiple of 1/4 below 2^6 and the scales are powers of two, so the fp32 accumulation is
 // exact but for scales that lie many powers of two apart.
-// Persistent CTAs over tiles of 128 rows x kN columns.  Warp 0 loads (A and B as bytes in rows of 128 = 256 elements of K, 128B
-// swizzle; the scale tiles of both as they lie in memory), warp 1 copies the scales to tensor memory and issues the products
-// into one of two accumulators, warps 4 on are epilogue warpgroups, one per 64 columns, which add the bias, round once and
-// store through shared memory.  The products of the next tile run under the epilogue of this one.
+// Persistent CTAs over tiles of 128 rows x 64 or 128 columns, or pairs of CTAs (cta_group::2, half of A's and of B's rows
+// each) over tiles of 256 x 256.  Warp 0 loads A and B as bytes (rows of 128 = 256 elements of K, 128B swizzle), warp 2 the scale
+// tiles of both as they lie in memory, warp 1 copies the scales to tensor memory and issues the products into one of two
+// accumulators, warps 4 on are epilogue warpgroups, one per 64 columns, which add the bias, round once and store through
+// shared memory.  The products of the next tile run under the epilogue of this one.
+// Tensor memory: two accumulators of 256 columns leave no room for the scales, so they share 32 columns: the warpgroup that
+// has these reads them first, and the next tile's products wait for that (a few hundred cycles) and not for the epilogue.
 // Every mbarrier wait is bounded; on expiry the CTA sets *device_status and its roles leave their loops.
 #include <algorithm>
 
@@ -26,33 +29,39 @@ constexpr int kMaxStages = 5;
 
 template <int kN>
 struct Layout {
+  static constexpr bool kPair = kN == 256;
+  static constexpr int kCtas = kPair ? 2 : 1;
   static constexpr int kGroups = kN / 64;                      // epilogue warpgroups
   static constexpr int kThreads = 128 + 128 * kGroups;
-  static constexpr int kStages = 5;
+  static constexpr int kStages = kPair ? 4 : 5;
+  static constexpr int kLoadN = kN / kCtas;                    // rows of B that this CTA loads
+  static constexpr int kTilesB = (kN + 127) / 128;             // scale tiles of B per 128 elements of K: of all columns in both CTAs
   static constexpr uint32_t kOffB = kTileM * kRowBytes;
-  static constexpr uint32_t kOffSfa = kOffB + kN * kRowBytes;  // two scale tiles of A, two of B
+  static constexpr uint32_t kOffSfa = kOffB + kLoadN * kRowBytes;  // two scale tiles of A, two for each 128 columns of B
   static constexpr uint32_t kOffSfb = kOffSfa + 2 * kScaleTile;
-  static constexpr uint32_t kStageBytes = kOffSfb + 2 * kScaleTile;
+  static constexpr uint32_t kScaleBytes = (2 + 2 * kTilesB) * kScaleTile;
+  static constexpr uint32_t kStageBytes = kOffSfa + kScaleBytes;
   static constexpr uint32_t kOffOut = kStages * kStageBytes;   // staged output, 4 KB per epilogue warp
   static constexpr uint32_t kOffBias = kOffOut + kGroups * 16384;  // two sets by turns
   static constexpr uint32_t kOffBar = kOffBias + 2 * kN * 4;
   static constexpr uint32_t kSmemBytes = kOffBar + 256;
-  // tensor memory: two accumulators, then the scales of a stage for A (two columns groups of four) and B
-  static constexpr uint32_t kSfaCol = 2 * kN, kSfbCol = kSfaCol + 8;
+  // tensor memory: two accumulators, then the scales of a stage: four columns per scale tile
+  static constexpr uint32_t kShared = kPair ? 32 : 0;          // columns that the accumulators share
+  static constexpr uint32_t kAcc1 = kN - kShared;
+  static constexpr uint32_t kSfaCol = kAcc1 + kN, kSfbCol = kSfaCol + 8;
   static constexpr uint32_t kTmemCols = kN == 64 ? 256 : 512;
-  static_assert(kSfbCol + 8 <= kTmemCols && kStageBytes % 1024 == 0 && kSmemBytes <= 232448, "fits");
+  static_assert(kSfbCol + 8 * kTilesB <= kTmemCols && kStageBytes % 1024 == 0 && kSmemBytes <= 232448, "fits");
 };
 
 struct Bars {
   uint64_t full[kMaxStages], empty[kMaxStages];
   uint64_t acc_full[2], acc_empty[2];  // accumulator written (issuer -> epilogue) / read out (epilogue -> issuer)
+  uint64_t shared_read;                // the columns that both accumulators have are read out of this tile's
   uint32_t tmem_base;
   int abort;
 };
 
 struct MxParams {
-  const uint8_t* x_scales;
-  const uint8_t* w_scales;
   const float* bias;  // [d_out] or null
   int rows, d_in, d_out;
   int k_tiles;        // scale tiles along K
@@ -71,36 +80,47 @@ __device__ __forceinline__ void named_barrier_sync(int id, int threads) {
 template <int kN>
 __global__ void __launch_bounds__(Layout<kN>::kThreads, 1)
 linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_w,
+                   const __grid_constant__ CUtensorMap map_xs, const __grid_constant__ CUtensorMap map_ws,
                    const __grid_constant__ CUtensorMap map_y, const MxParams p) {
   using L = Layout<kN>;
-  constexpr int kStages = L::kStages;
+  constexpr int kStages = L::kStages, kCtas = L::kCtas;
+  constexpr bool kPair = L::kPair;
   extern __shared__ __align__(1024) uint8_t smem[];
   Bars* bars = reinterpret_cast<Bars*>(smem + L::kOffBar);
   volatile int* abort_flag = &bars->abort;
-  if ((smem_u32(smem) & 1023u) != 0) {
+  if ((smem_u32(smem) & 1023u) != 0) {  // the same in both CTAs of a pair
     if (threadIdx.x == 0 && p.status != nullptr) atomicCAS(p.status, 0, 900);
     return;
   }
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int stages_k = (p.d_in + kStageK - 1) / kStageK;
+  const int rank = kPair ? static_cast<int>(cluster_rank()) : 0;
+  const int first_tile = blockIdx.x / kCtas, tile_step = gridDim.x / kCtas;
 
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) {
-      mbar_init(&bars->full[s], 1);
+      mbar_init(&bars->full[s], 2);  // operands, scales
       mbar_init(&bars->empty[s], 1);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&bars->acc_full[b], 1);
-      mbar_init(&bars->acc_empty[b], L::kGroups * 4);
+      mbar_init(&bars->acc_empty[b], kCtas * L::kGroups * 4);
     }
+    mbar_init(&bars->shared_read, kCtas * 4);
     bars->abort = 0;
     mbar_fence_init();
   }
   if (warp == 1) {
-    tmem_alloc(&bars->tmem_base, L::kTmemCols);
-    tmem_relinquish();
+    if constexpr (kPair) {
+      tmem_alloc_pair(&bars->tmem_base, L::kTmemCols);
+      tmem_relinquish_pair();
+    } else {
+      tmem_alloc(&bars->tmem_base, L::kTmemCols);
+      tmem_relinquish();
+    }
   }
   tc_fence_before();
+  if constexpr (kPair) cluster_sync();  // barriers and tensor memory of both CTAs are there
   __syncthreads();
   tc_fence_after();
   const uint32_t tmem = bars->tmem_base;
@@ -108,44 +128,57 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
   launch_dependents();
   if (blockIdx.x == 0 && threadIdx.x == 0 && p.status != nullptr) *p.status = 0;
 
-  if (warp == 0) {
+  if (warp == 0 || warp == 2) {
     if (lane == 0) {
-      tma_prefetch_desc(&map_x);
-      tma_prefetch_desc(&map_w);
+      const bool operands = warp == 0;
+      tma_prefetch_desc(operands ? &map_x : &map_xs);
+      tma_prefetch_desc(operands ? &map_w : &map_ws);
+      constexpr uint32_t kOperandBytes = L::kOffSfa;
       bool ok = true;
       int kc = 0;
-      for (int tile = blockIdx.x; ok && tile < p.tiles; tile += gridDim.x) {
+      for (int tile = first_tile; ok && tile < p.tiles; tile += tile_step) {
         const int row_tile = tile / p.col_tiles, col0 = (tile - row_tile * p.col_tiles) * kN;
+        const int row0 = (row_tile * kCtas + rank) * kTileM;
         for (int k = 0; ok && k < stages_k; ++k, ++kc) {
           const int st = kc % kStages;
           if (kc >= kStages)
-            ok = mbar_wait_clearing(&bars->empty[st], ((kc - kStages) / kStages) & 1, abort_flag, p.status, 801, 32);
+            ok = mbar_wait_clearing(&bars->empty[st], ((kc - kStages) / kStages) & 1, abort_flag, p.status, 801);
           if (!ok) break;
           uint8_t* const dst = smem + st * L::kStageBytes;
-          const int scale_tiles = min(2, p.k_tiles - 2 * k);  // the last stage may have one
-          const uint32_t scale_bytes = static_cast<uint32_t>(scale_tiles) * kScaleTile;
-          mbar_arrive_expect_tx(&bars->full[st], (kTileM + kN) * kRowBytes + 2 * scale_bytes);
-          tma_load_2d(dst, &map_x, &bars->full[st], k * kRowBytes, row_tile * kTileM);
-          tma_load_2d(dst + L::kOffB, &map_w, &bars->full[st], k * kRowBytes, col0);
-          bulk_load(dst + L::kOffSfa, p.x_scales + (static_cast<size_t>(row_tile) * p.k_tiles + 2 * k) * kScaleTile, scale_bytes, &bars->full[st]);
-          bulk_load(dst + L::kOffSfb, p.w_scales + (static_cast<size_t>(col0 / 128) * p.k_tiles + 2 * k) * kScaleTile, scale_bytes, &bars->full[st]);
+          // both CTAs' loads count on the first one's barrier
+          if (rank == 0) mbar_arrive_expect_tx(&bars->full[st], kCtas * (operands ? kOperandBytes : L::kScaleBytes));
+          auto load = [&](uint32_t off, const CUtensorMap* map, int x, int y) {
+            if constexpr (kPair) tma_load_2d_pair(dst + off, map, cluster_u32(&bars->full[st], 0), x, y);
+            else tma_load_2d(dst + off, map, &bars->full[st], x, y);
+          };
+          if (operands) {
+            load(0, &map_x, k * kRowBytes, row0);
+            load(L::kOffB, &map_w, k * kRowBytes, col0 + rank * L::kLoadN);
+          } else {  // two neighbouring scale tiles (the second unused at the end of an odd number of them)
+            load(L::kOffSfa, &map_xs, 0, (row_tile * kCtas + rank) * p.k_tiles + 2 * k);
+#pragma unroll
+            for (int b = 0; b < L::kTilesB; ++b)
+              load(L::kOffSfb + b * 2 * kScaleTile, &map_ws, 0, (col0 / 128 + b) * p.k_tiles + 2 * k);
+          }
         }
       }
     }
   } else if (warp == 1) {
-    if (lane == 0) {
+    if (lane == 0 && rank == 0) {
+      constexpr uint32_t idesc0 = instr_desc_mxf4(kCtas * kTileM, kN, 0), idesc2 = instr_desc_mxf4(kCtas * kTileM, kN, 2);
       const uint64_t a_desc0 = smem_desc(smem_u32(smem), 16, 1024, kSwizzle128);
       const uint64_t b_desc0 = smem_desc(smem_u32(smem) + L::kOffB, 16, 1024, kSwizzle128);
-      const uint64_t sfa_desc0 = smem_desc(smem_u32(smem) + L::kOffSfa, 16, 128, 0);
-      const uint64_t sfb_desc0 = smem_desc(smem_u32(smem) + L::kOffSfb, 16, 128, 0);
+      const uint64_t s_desc0 = smem_desc(smem_u32(smem) + L::kOffSfa, 16, 128, 0);
       const int products = (p.d_in + 63) / 64;
       bool ok = true;
       int kc = 0, it = 0;
-      for (int tile = blockIdx.x; ok && tile < p.tiles; tile += gridDim.x, ++it) {
+      for (int tile = first_tile; ok && tile < p.tiles; tile += tile_step, ++it) {
         const int ab = it & 1;
+        const uint32_t acc = tmem + (ab ? L::kAcc1 : 0u);
         // with tiles of 64 columns the weight's scale tile serves two of them: columns 0 and 1, or 2 and 3
         const uint32_t sfb_shift = kN == 64 ? 2u * ((tile % p.col_tiles) & 1) : 0u;
         if (it >= 2) ok = mbar_wait_clearing(&bars->acc_empty[ab], ((it - 2) >> 1) & 1, abort_flag, p.status, 804);
+        if (L::kShared != 0 && ok && it >= 1) ok = mbar_wait_clearing(&bars->shared_read, (it - 1) & 1, abort_flag, p.status, 805);
         tc_fence_after();
         for (int k = 0; ok && k < stages_k; ++k, ++kc) {
           const int st = kc % kStages;
@@ -154,20 +187,34 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
           tc_fence_after();
           const uint64_t off = static_cast<uint64_t>((st * L::kStageBytes) >> 4);
           const int todo = min(4, products - 4 * k);
-          for (int t = 0; t < (todo + 1) / 2; ++t) {
-            tmem_copy_scales(tmem + L::kSfaCol + 4 * t, sfa_desc0 + off + ((t * kScaleTile) >> 4));
-            tmem_copy_scales(tmem + L::kSfbCol + 4 * t, sfb_desc0 + off + ((t * kScaleTile) >> 4));
+          auto copy = [&](uint32_t col, uint32_t smem_off) {
+            if constexpr (kPair) tmem_copy_scales_pair(tmem + col, s_desc0 + off + (smem_off >> 4));
+            else tmem_copy_scales(tmem + col, s_desc0 + off + (smem_off >> 4));
+          };
+#pragma unroll
+          for (int t = 0; t < 2; ++t) {
+            if (2 * t >= todo) break;
+            copy(L::kSfaCol + 4 * t, t * kScaleTile);
+#pragma unroll
+            for (int b = 0; b < L::kTilesB; ++b)
+              copy(L::kSfbCol + 4 * (t * L::kTilesB + b), (2 + 2 * b + t) * kScaleTile);
           }
 #pragma unroll
           for (int kk = 0; kk < 4; ++kk) {
             if (kk >= todo) break;
-            const uint32_t idesc = (kk & 1) ? instr_desc_mxf4(kTileM, kN, 2) : instr_desc_mxf4(kTileM, kN, 0);
-            mma_mxf4(tmem + ab * kN, a_desc0 + off + ((kk * 32) >> 4), b_desc0 + off + ((kk * 32) >> 4), idesc,
-                     tmem + L::kSfaCol + 4 * (kk >> 1), tmem + L::kSfbCol + 4 * (kk >> 1) + sfb_shift, (k > 0 || kk > 0) ? 1u : 0u);
+            const uint64_t a_desc = a_desc0 + off + ((kk * 32) >> 4), b_desc = b_desc0 + off + ((kk * 32) >> 4);
+            const uint32_t sfa = tmem + L::kSfaCol + 4 * (kk >> 1), sfb = tmem + L::kSfbCol + 4 * L::kTilesB * (kk >> 1) + sfb_shift;
+            const uint32_t accumulate = (k > 0 || kk > 0) ? 1u : 0u;
+            if constexpr (kPair) mma_mxf4_pair(acc, a_desc, b_desc, (kk & 1) ? idesc2 : idesc0, sfa, sfb, accumulate);
+            else mma_mxf4(acc, a_desc, b_desc, (kk & 1) ? idesc2 : idesc0, sfa, sfb, accumulate);
           }
-          mma_commit(&bars->empty[st]);
+          if constexpr (kPair) mma_commit_pair(&bars->empty[st]);
+          else mma_commit(&bars->empty[st]);
         }
-        if (ok) mma_commit(&bars->acc_full[ab]);
+        if (ok) {
+          if constexpr (kPair) mma_commit_pair(&bars->acc_full[ab]);
+          else mma_commit(&bars->acc_full[ab]);
+        }
       }
     }
   } else if (warp >= 4) {
@@ -180,11 +227,11 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     const bool wide = p.y_dtype == LITE3R_F32;
     bool ok = true;
     int it = 0;
-    for (int tile = blockIdx.x; ok && tile < p.tiles; tile += gridDim.x, ++it) {
+    for (int tile = first_tile; ok && tile < p.tiles; tile += tile_step, ++it) {
       const int ab = it & 1;
       const int row_tile = tile / p.col_tiles;
-      const int row0 = row_tile * kTileM, col = (tile - row_tile * p.col_tiles) * kN + hh * 64;
-      const uint32_t acc_addr = tmem + ((static_cast<uint32_t>(quarter) * 32u) << 16) + ab * kN + hh * 64;
+      const int row0 = (row_tile * kCtas + rank) * kTileM, col = (tile - row_tile * p.col_tiles) * kN + hh * 64;
+      const uint32_t acc_addr = tmem + ((static_cast<uint32_t>(quarter) * 32u) << 16) + (ab ? L::kAcc1 : 0u) + hh * 64;
       float* const bia = reinterpret_cast<float*>(smem + L::kOffBias) + ab * kN + hh * 64;
       if (tid < 64) bia[tid] = (p.bias != nullptr && col + tid < p.d_out) ? __ldg(p.bias + col + tid) : 0.f;
       named_barrier_sync(1 + hh, 128);
@@ -192,28 +239,37 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
       tc_fence_after();
       ok = __all_sync(0xFFFFFFFFu, ok);
       if (!ok) break;
-      auto acc_read_out = [&] {
+      auto read_out = [&](uint64_t* bar) {  // the issuer waits in the first CTA
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(&bars->acc_empty[ab]);
+        if (lane == 0) {
+          if constexpr (kPair) mbar_arrive_cluster(cluster_u32(bar, 0));
+          else mbar_arrive(bar);
+        }
       };
+      // the shared columns are the first accumulator's last and the second one's first: this warpgroup reads them first
+      const bool shares = L::kShared != 0 && hh == (ab ? 0 : L::kGroups - 1);
       if (col >= p.d_out) {
-        acc_read_out();
+        if (shares) read_out(&bars->shared_read);
+        read_out(&bars->acc_empty[ab]);
         continue;
       }
       // The warp stages its 32 rows, 128 bytes at a time, in the layout the store engine reads (128B swizzle); rows and
       // columns past the output are clipped by the engine, columns at 16 bytes: a ragged end is stored value by value.
       const bool ragged = p.ragged && col + 64 > p.d_out;
+      const int first_cb = shares && ab == 0 ? 32 : 0;
 #pragma unroll 1
-      for (int cb = 0; cb < 64; cb += 32) {
+      for (int j = 0; j < 2; ++j) {
+        const int cb = j == 0 ? first_cb : 32 - first_cb;
         uint32_t v[32];
         tmem_ld32(acc_addr + cb, v);
-        if (wide || cb == 0) {  // what was staged here before has been read by the store engine
+        if (wide || j == 0) {  // what was staged here before has been read by the store engine
           if (lane == 0) bulk_wait_group_read0();
           __syncwarp();
         }
         tmem_wait_ld();
-        if (cb == 32) acc_read_out();
+        if (shares && j == 0) read_out(&bars->shared_read);
+        if (j == 1) read_out(&bars->acc_empty[ab]);
 #pragma unroll
         for (int c = 0; c < 32; c += 4) {
           const float4 b4 = *reinterpret_cast<const float4*>(bia + cb + c);
@@ -257,7 +313,7 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             sts128(my_row + (((cb / 8 + c) ^ swz) << 4), w[0], w[1], w[2], w[3]);
           }
         }
-        if (wide || cb == 32) {
+        if (wide || j == 1) {
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
@@ -273,31 +329,46 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
   tc_fence_before();
   __syncthreads();
   linger_after_abort(abort_flag);
+  if constexpr (kPair) cluster_sync();  // neither CTA leaves while the other one's loads, products or arrivals may reach it
   if (warp == 1) {
     tc_fence_after();
-    tmem_dealloc(tmem, L::kTmemCols);
+    if constexpr (kPair) tmem_dealloc_pair(tmem, L::kTmemCols);
+    else tmem_dealloc(tmem, L::kTmemCols);
   }
 }
 
+struct Operands {
+  const uint8_t *x_codes, *x_scales, *w_codes, *w_scales;
+};
+
+// Scale tiles as rows of 128 words, two of them to a box.
+lite3r_status scale_map(CUtensorMap* map, const uint8_t* scales, int rows, int k_tiles) {
+  return make_tensor_map_2d(map, CU_TENSOR_MAP_DATA_TYPE_UINT32, 4, scales, 128, static_cast<uint64_t>(ceil_div(rows, 128)) * k_tiles, 128, 2,
+                            CU_TENSOR_MAP_SWIZZLE_NONE);
+}
+
 template <int kN>
-lite3r_status launch_tiles(const uint8_t* x_codes, const uint8_t* w_codes, const CUtensorMap& map_y, const MxParams& p, int sms,
-                           cudaStream_t stream) {
+lite3r_status launch_tiles(const Operands& o, const CUtensorMap& map_y, const MxParams& p, int sms, cudaStream_t stream) {
   using L = Layout<kN>;
-  CUtensorMap map_x, map_w;
+  CUtensorMap map_x, map_w, map_xs, map_ws;
   lite3r_status st;
   const uint64_t pitch = static_cast<uint64_t>(p.d_in) / 2;
-  if ((st = make_tensor_map_2d(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, x_codes, pitch, p.rows, kRowBytes, kTileM,
+  if ((st = make_tensor_map_2d(&map_x, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, o.x_codes, pitch, p.rows, kRowBytes, kTileM,
                                CU_TENSOR_MAP_SWIZZLE_128B)) != LITE3R_OK) return st;
-  if ((st = make_tensor_map_2d(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, w_codes, pitch, p.d_out, kRowBytes, kN,
+  if ((st = make_tensor_map_2d(&map_w, CU_TENSOR_MAP_DATA_TYPE_UINT8, 1, o.w_codes, pitch, p.d_out, kRowBytes, L::kLoadN,
                                CU_TENSOR_MAP_SWIZZLE_128B)) != LITE3R_OK) return st;
+  if ((st = scale_map(&map_xs, o.x_scales, p.rows, p.k_tiles)) != LITE3R_OK) return st;
+  if ((st = scale_map(&map_ws, o.w_scales, p.d_out, p.k_tiles)) != LITE3R_OK) return st;
   if ((st = ensure_dynamic_smem(linear_mxf4_kernel<kN>, static_cast<int>(L::kSmemBytes))) != LITE3R_OK) return st;
   MxParams q = p;
   q.col_tiles = ceil_div(p.d_out, kN);
-  const long long tiles = static_cast<long long>(q.col_tiles) * ceil_div(p.rows, kTileM);
-  if (tiles > 0x7FFFFFFFLL - 1024) return LITE3R_ERR_UNSUPPORTED;
+  const long long tiles = static_cast<long long>(q.col_tiles) * ceil_div(p.rows, L::kCtas * kTileM);
+  // (coordinates of scale tiles and tile numbers are 32-bit)
+  if (tiles > 0x7FFFFFFFLL - 1024 || static_cast<long long>(ceil_div(std::max(p.rows, p.d_out), 128) + 2) * p.k_tiles > 0x7FFFFFFFLL)
+    return LITE3R_ERR_UNSUPPORTED;
   q.tiles = static_cast<int>(tiles);
-  return launch_dependent(linear_mxf4_kernel<kN>, dim3(static_cast<unsigned>(std::min(q.tiles, sms))), L::kThreads,
-                          static_cast<int>(L::kSmemBytes), stream, map_x, map_w, map_y, q);
+  return launch_dependent_cluster(linear_mxf4_kernel<kN>, dim3(static_cast<unsigned>(L::kCtas * std::min(q.tiles, sms / L::kCtas))), L::kThreads,
+                                  static_cast<int>(L::kSmemBytes), L::kCtas, stream, map_x, map_w, map_xs, map_ws, map_y, q);
 }
 
 }  // namespace
@@ -308,9 +379,8 @@ lite3r_status launch_linear_mxf4(const uint8_t* x_codes, const uint8_t* x_scales
   int sms = 0;
   lite3r_status st = sm_count(&sms);
   if (st != LITE3R_OK) return st;
+  const Operands o = {x_codes, x_scales, w_codes, w_scales};
   MxParams p = {};
-  p.x_scales = x_scales;
-  p.w_scales = w_scales;
   p.bias = bias;
   p.rows = rows;
   p.d_in = d_in;
@@ -329,9 +399,10 @@ lite3r_status launch_linear_mxf4(const uint8_t* x_codes, const uint8_t* x_scales
                                                    : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
                           elem, y, d_out, rows, 128 / elem, 32, CU_TENSOR_MAP_SWIZZLE_128B, static_cast<uint64_t>(y_stride) * elem);
   if (st != LITE3R_OK) return st;
-  return static_cast<long long>(ceil_div(d_out, 128)) * ceil_div(rows, kTileM) < sms
-             ? launch_tiles<64>(x_codes, w_codes, map_y, p, sms, stream)
-             : launch_tiles<128>(x_codes, w_codes, map_y, p, sms, stream);
+  // Pairs on 256 x 256 from more than one such tile for every two pairs; below that more and smaller tiles use more SMs.
+  const long long row_tiles = ceil_div(rows, kTileM);
+  if (static_cast<long long>(ceil_div(d_out, 256)) * ceil_div(rows, 256) > sms / 4) return launch_tiles<256>(o, map_y, p, sms, stream);
+  return ceil_div(d_out, 128) * row_tiles < sms ? launch_tiles<64>(o, map_y, p, sms, stream) : launch_tiles<128>(o, map_y, p, sms, stream);
 }
 
 }  // namespace lite3r

@@ -35,8 +35,12 @@ def workspace(nbytes):
 
 
 def within(got, ref, tol, dtype, what):
-    got = f64(got)
-    assert np.isfinite(got).all(), what
+    """Values that round beyond the type's largest (fp16: from 65520 = 65504 + half a step on) have to be infinite."""
+    got, tol = f64(got), np.broadcast_to(tol, ref.shape)
+    end = torch.finfo(dtype).max * (1 + HALF_STEP[dtype] / (2 - 2 * HALF_STEP[dtype]))
+    over, under = np.abs(ref) - tol >= end, np.abs(ref) + tol < end
+    assert (got[over] == np.sign(ref[over]) * np.inf).all() and np.isfinite(got[under]).all(), what
+    got, ref, tol = got[under], ref[under], tol[under]
     tol = tol + HALF_STEP[dtype] * (np.abs(ref) + tol) + TINY[dtype]
     worst = (np.abs(got - ref) / np.maximum(tol, 1e-300)).max() if got.size else 0.0
     assert worst <= 1.0, (what, worst)
@@ -319,7 +323,7 @@ def mx_matrix(seed, rows, cols, fmt, spread=1.0):
 
 LINEAR_CASES = [(1, 32, 1, "f32", True), (70, 64, 9, "bf16", True), (33, 160, 131, "f16", True), (1, 1024, 1024, "bf16", True), (129, 96, 65, "f32", True), (300, 1184, 1000, "f32", False),
                 (513, 2048, 136, "f16", True), (128, 64, 8, "bf16", False), (17, 128, 4096, "f32", True), (2000, 416, 1300, "bf16", True),
-                (130, 544, 320, "f32", True)]
+                (130, 544, 320, "f32", True), (10007, 288, 1003, "bf16", True), (5001, 544, 2056, "f32", False), (9000, 1120, 648, "f16", True)]
 
 
 @pytest.mark.parametrize("rows,d_in,d_out,dtype,with_bias", LINEAR_CASES)
