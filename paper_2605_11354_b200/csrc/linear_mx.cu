@@ -164,7 +164,10 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
+    // The loop runs in all lanes and one of them issues: descriptors then stay in uniform registers (worked out by one lane
+    // they left 40 idle cycles between two products of 128).
+    if (rank == 0) {
+      const bool issuer = elect_one();
       constexpr uint32_t idesc0 = instr_desc_mxf4(kCtas * kTileM, kN, 0), idesc2 = instr_desc_mxf4(kCtas * kTileM, kN, 2);
       const uint64_t a_desc0 = smem_desc(smem_u32(smem), 16, 1024, kSwizzle128);
       const uint64_t b_desc0 = smem_desc(smem_u32(smem) + L::kOffB, 16, 1024, kSwizzle128);
@@ -187,31 +190,33 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
           tc_fence_after();
           const uint64_t off = static_cast<uint64_t>((st * L::kStageBytes) >> 4);
           const int todo = min(4, products - 4 * k);
-          auto copy = [&](uint32_t col, uint32_t smem_off) {
-            if constexpr (kPair) tmem_copy_scales_pair(tmem + col, s_desc0 + off + (smem_off >> 4));
-            else tmem_copy_scales(tmem + col, s_desc0 + off + (smem_off >> 4));
-          };
+          if (issuer) {
+            auto copy = [&](uint32_t col, uint32_t smem_off) {
+              if constexpr (kPair) tmem_copy_scales_pair(tmem + col, s_desc0 + off + (smem_off >> 4));
+              else tmem_copy_scales(tmem + col, s_desc0 + off + (smem_off >> 4));
+            };
 #pragma unroll
-          for (int t = 0; t < 2; ++t) {
-            if (2 * t >= todo) break;
-            copy(L::kSfaCol + 4 * t, t * kScaleTile);
+            for (int t = 0; t < 2; ++t) {
+              if (2 * t >= todo) break;
+              copy(L::kSfaCol + 4 * t, t * kScaleTile);
 #pragma unroll
-            for (int b = 0; b < L::kTilesB; ++b)
-              copy(L::kSfbCol + 4 * (t * L::kTilesB + b), (2 + 2 * b + t) * kScaleTile);
+              for (int b = 0; b < L::kTilesB; ++b)
+                copy(L::kSfbCol + 4 * (t * L::kTilesB + b), (2 + 2 * b + t) * kScaleTile);
+            }
+#pragma unroll
+            for (int kk = 0; kk < 4; ++kk) {
+              if (kk >= todo) break;
+              const uint64_t a_desc = a_desc0 + off + ((kk * 32) >> 4), b_desc = b_desc0 + off + ((kk * 32) >> 4);
+              const uint32_t sfa = tmem + L::kSfaCol + 4 * (kk >> 1), sfb = tmem + L::kSfbCol + 4 * L::kTilesB * (kk >> 1) + sfb_shift;
+              const uint32_t accumulate = (k > 0 || kk > 0) ? 1u : 0u;
+              if constexpr (kPair) mma_mxf4_pair(acc, a_desc, b_desc, (kk & 1) ? idesc2 : idesc0, sfa, sfb, accumulate);
+              else mma_mxf4(acc, a_desc, b_desc, (kk & 1) ? idesc2 : idesc0, sfa, sfb, accumulate);
+            }
+            if constexpr (kPair) mma_commit_pair(&bars->empty[st]);
+            else mma_commit(&bars->empty[st]);
           }
-#pragma unroll
-          for (int kk = 0; kk < 4; ++kk) {
-            if (kk >= todo) break;
-            const uint64_t a_desc = a_desc0 + off + ((kk * 32) >> 4), b_desc = b_desc0 + off + ((kk * 32) >> 4);
-            const uint32_t sfa = tmem + L::kSfaCol + 4 * (kk >> 1), sfb = tmem + L::kSfbCol + 4 * L::kTilesB * (kk >> 1) + sfb_shift;
-            const uint32_t accumulate = (k > 0 || kk > 0) ? 1u : 0u;
-            if constexpr (kPair) mma_mxf4_pair(acc, a_desc, b_desc, (kk & 1) ? idesc2 : idesc0, sfa, sfb, accumulate);
-            else mma_mxf4(acc, a_desc, b_desc, (kk & 1) ? idesc2 : idesc0, sfa, sfb, accumulate);
-          }
-          if constexpr (kPair) mma_commit_pair(&bars->empty[st]);
-          else mma_commit(&bars->empty[st]);
         }
-        if (ok) {
+        if (ok && issuer) {
           if constexpr (kPair) mma_commit_pair(&bars->acc_full[ab]);
           else mma_commit(&bars->acc_full[ab]);
         }

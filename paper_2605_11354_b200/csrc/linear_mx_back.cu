@@ -246,10 +246,14 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
       }
     }
   } else if (warp == 1) {
-    if (lane == 0 && rank == 0) {
+    // The loop runs in all lanes and one of them issues: descriptors then stay in uniform registers (worked out by one lane
+    // they left 40 idle cycles between two products of 128).
+    if (rank == 0) {
+      const bool issuer = elect_one();
       constexpr uint32_t idesc_wide = instr_desc(1, kTileM, kTileN, kWgrad ? 1 : 0, 1);
       constexpr uint32_t idesc_half = instr_desc(1, kTileM, kTileN / 2, kWgrad ? 1 : 0, 1);
-      const uint32_t base = smem_u32(smem);
+      const uint64_t a_desc0 = kWgrad ? smem_desc(smem_u32(smem), 8192, 1024, kSwizzle128) : smem_desc(smem_u32(smem), 16, 1024, kSwizzle128);
+      const uint64_t b_desc0 = smem_desc(smem_u32(smem) + L::kOffB, 8192, 1024, kSwizzle128);
       bool ok = true;
       int kc = 0, it = 0;
       for (int unit = first_unit; ok && unit < p.units; unit += unit_step) {
@@ -264,15 +268,16 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
             ok = mbar_wait_cluster_clearing(&bars->b_full[st], (kc / kOps) & 1, abort_flag, p.status, 816);
             if (!ok) break;
             tc_fence_after();
-            const uint32_t a = base + st * L::kOpBytes, b = a + L::kOffB;
+            if (issuer) {
+              const uint64_t off = static_cast<uint64_t>((st * L::kOpBytes) >> 4);
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {  // 16 steps of the contraction each
-              const uint64_t a_desc = kWgrad ? smem_desc(a + kk * 2048, 8192, 1024, kSwizzle128) : smem_desc(a + kk * 32, 16, 1024, kSwizzle128);
-              mma_f16_pair(tmem + ab * kTileN, a_desc, smem_desc(b + kk * 2048, 8192, 1024, kSwizzle128), idesc, (k > k0 || kk > 0) ? 1u : 0u);
+              for (int kk = 0; kk < 4; ++kk)  // 16 steps of the contraction each
+                mma_f16_pair(tmem + ab * kTileN, a_desc0 + off + kk * ((kWgrad ? 2048 : 32) >> 4), b_desc0 + off + kk * (2048 >> 4), idesc,
+                             (k > k0 || kk > 0) ? 1u : 0u);
+              mma_commit_pair(&bars->op_empty[st]);
             }
-            mma_commit_pair(&bars->op_empty[st]);
           }
-          if (ok) mma_commit_pair(&bars->acc_full[ab]);
+          if (ok && issuer) mma_commit_pair(&bars->acc_full[ab]);
         }
       }
     }
