@@ -39,7 +39,14 @@ __device__ __forceinline__ float byte_to_scale(uint32_t byte) {  // 2^(byte - 12
   return byte == 0xFFu ? __uint_as_float(0x7FFFFFFFu) : __uint_as_float(byte == 0u ? 0x00400000u : byte << 23);
 }
 
-// Eight values as they lie in memory and the largest of their magnitudes as fp32 bits (NaN above infinity above all else).
+__device__ __forceinline__ float max_nan(float a, float b) {
+  float m;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+  return m;
+}
+
+// Eight values as they lie in memory, and the largest magnitude of them and of the three neighbouring lanes (a block) as fp32
+// bits: NaN above infinity above all else.
 template <typename T>
 struct Octet;
 template <>
@@ -50,59 +57,122 @@ struct Octet<float> {
     b = __ldg(reinterpret_cast<const float4*>(p) + 1);
   }
   __device__ __forceinline__ void clear() { a = b = make_float4(0.f, 0.f, 0.f, 0.f); }
-  __device__ __forceinline__ void values(float v[8]) const {
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
-    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  __device__ __forceinline__ void pairs(uint64_t v[4]) const {
+    v[0] = pack_f32x2(a.x, a.y); v[1] = pack_f32x2(a.z, a.w);
+    v[2] = pack_f32x2(b.x, b.y); v[3] = pack_f32x2(b.z, b.w);
   }
-  __device__ __forceinline__ uint32_t top() const {
-    float v[8];
-    values(v);
-    uint32_t m = 0;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) m = max(m, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-    return m;
+  __device__ __forceinline__ uint32_t block_top() const {
+    float m = max_nan(max_nan(max_nan(fabsf(a.x), fabsf(a.y)), max_nan(fabsf(a.z), fabsf(a.w))),
+                      max_nan(max_nan(fabsf(b.x), fabsf(b.y)), max_nan(fabsf(b.z), fabsf(b.w))));
+    m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, 1));
+    m = max_nan(m, __shfl_xor_sync(0xFFFFFFFFu, m, 2));
+    return __float_as_uint(m) & 0x7FFFFFFFu;
   }
 };
-template <typename T>
+// The 16-bit types, two values at a time (H2: __nv_bfloat162 or __half2).
+template <typename T, typename H2>
 struct Octet16 {
   uint4 w;
   __device__ __forceinline__ void load(const T* p) { w = __ldg(reinterpret_cast<const uint4*>(p)); }
   __device__ __forceinline__ void clear() { w = make_uint4(0u, 0u, 0u, 0u); }
-  __device__ __forceinline__ uint32_t top16() const {  // the largest magnitude's 16 bits
-    constexpr uint32_t kAbs = 0x7FFF7FFFu;
-    const uint32_t m = __vmaxu2(__vmaxu2(w.x & kAbs, w.y & kAbs), __vmaxu2(w.z & kAbs, w.w & kAbs));
-    return max(m & 0xFFFFu, m >> 16);
+  static __device__ __forceinline__ H2 two(uint32_t x) { return *reinterpret_cast<const H2*>(&x); }
+  static __device__ __forceinline__ uint32_t bits(H2 x) { return *reinterpret_cast<const uint32_t*>(&x); }
+  __device__ __forceinline__ uint32_t block_top16() const {
+    H2 m = __hmax2_nan(__hmax2_nan(__habs2(two(w.x)), __habs2(two(w.y))), __hmax2_nan(__habs2(two(w.z)), __habs2(two(w.w))));
+    m = __hmax2_nan(m, two(__shfl_xor_sync(0xFFFFFFFFu, bits(m), 1)));
+    m = __hmax2_nan(m, two(__shfl_xor_sync(0xFFFFFFFFu, bits(m), 2)));
+    return bits(__hmax2_nan(m, __lowhigh2highlow(m))) & 0x7FFFu;
   }
 };
 template <>
-struct Octet<__nv_bfloat16> : Octet16<__nv_bfloat16> {
-  __device__ __forceinline__ void values(float v[8]) const {
+struct Octet<__nv_bfloat16> : Octet16<__nv_bfloat16, __nv_bfloat162> {
+  __device__ __forceinline__ void pairs(uint64_t v[4]) const {
     const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(x[i] << 16);
-      v[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
-    }
+    for (int i = 0; i < 4; ++i) v[i] = pack_f32x2(__uint_as_float(x[i] << 16), __uint_as_float(x[i] & 0xFFFF0000u));
   }
-  __device__ __forceinline__ uint32_t top() const { return top16() << 16; }
+  __device__ __forceinline__ uint32_t block_top() const { return block_top16() << 16; }
 };
 template <>
-struct Octet<__half> : Octet16<__half> {
-  __device__ __forceinline__ void values(float v[8]) const {
+struct Octet<__half> : Octet16<__half, __half2> {
+  __device__ __forceinline__ void pairs(uint64_t v[4]) const {
     const uint32_t x[4] = {w.x, w.y, w.z, w.w};
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float2 f = __half22float2(*reinterpret_cast<const __half2*>(&x[i]));
-      v[2 * i] = f.x;
-      v[2 * i + 1] = f.y;
+      const float2 f = __half22float2(two(x[i]));
+      v[i] = pack_f32x2(f.x, f.y);
     }
   }
-  __device__ __forceinline__ uint32_t top() const { return __float_as_uint(__half2float(__ushort_as_half(static_cast<unsigned short>(top16())))); }
+  __device__ __forceinline__ uint32_t block_top() const {
+    return __float_as_uint(__half2float(__ushort_as_half(static_cast<unsigned short>(block_top16()))));
+  }
 };
+
+// Four pairs of values to codes.
+__device__ __forceinline__ uint32_t e2m1x8(const uint64_t v[4]) {
+  float a[8];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) unpack_f32x2(v[i], a[2 * i], a[2 * i + 1]);
+  uint32_t r;
+  asm("{\n\t.reg .b8 b0, b1, b2, b3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b0, %2, %1;\n\tcvt.rn.satfinite.e2m1x2.f32 b1, %4, %3;\n\t"
+      "cvt.rn.satfinite.e2m1x2.f32 b2, %6, %5;\n\tcvt.rn.satfinite.e2m1x2.f32 b3, %8, %7;\n\t"
+      "mov.b32 %0, {b0, b1, b2, b3};\n\t}"
+      : "=r"(r)
+      : "f"(a[0]), "f"(a[1]), "f"(a[2]), "f"(a[3]), "f"(a[4]), "f"(a[5]), "f"(a[6]), "f"(a[7]));
+  return r;
+}
+__device__ __forceinline__ uint32_t e4m3x4(uint64_t x, uint64_t y) {
+  float a, b, c, d;
+  unpack_f32x2(x, a, b);
+  unpack_f32x2(y, c, d);
+  uint32_t r;
+  asm("{\n\t.reg .b16 lo, hi;\n\tcvt.rn.satfinite.e4m3x2.f32 lo, %2, %1;\n\tcvt.rn.satfinite.e4m3x2.f32 hi, %4, %3;\n\t"
+      "mov.b32 %0, {lo, hi};\n\t}"
+      : "=r"(r)
+      : "f"(a), "f"(b), "f"(c), "f"(d));
+  return r;
+}
 
 // Row pitch of the codes in bytes.
 template <int kFormat>
 __device__ __forceinline__ size_t code_pitch(int cols) { return kFormat == LITE3R_MXFP4 ? cols / 2 : cols; }
+
+// A thread's eight values of every sixteenth row of a tile; rows and cols are those of the tile inside the matrix, kFull: all.
+template <typename T, int kFormat, bool kFull>
+__device__ __forceinline__ void quantise_tile(const T* __restrict__ x, long long row_stride, int rows, int cols, uint8_t* __restrict__ codes,
+                                              size_t pitch, uint32_t scales_at, int r0, int lane16) {
+  Octet<T> in[kMxIters];
+#pragma unroll
+  for (int i = 0; i < kMxIters; ++i) {
+    if (kFull || (r0 + 16 * i < rows && lane16 * 8 < cols)) in[i].load(x + 16 * i * row_stride);
+    else in[i].clear();
+  }
+#pragma unroll
+  for (int i = 0; i < kMxIters; ++i) {
+    const uint32_t byte = scale_byte<kFormat>(in[i].block_top());
+    // row r0 + 16 i of the tile, r0 < 16
+    if ((lane16 & 3) == 0)
+      asm volatile("st.shared.u8 [%0], %1;" ::"r"(scales_at + (i & 1) * 256 + (i >> 1) * 4), "r"(byte) : "memory");
+    if (kFull || (r0 + 16 * i < rows && lane16 * 8 < cols)) {
+      const float inverse = __uint_as_float((254u << 23) - (byte << 23));  // (a block of NaN: whatever it is)
+      const uint64_t factor = pack_f32x2(inverse, inverse);
+      uint64_t v[4];
+      in[i].pairs(v);
+#pragma unroll
+      for (int q = 0; q < 4; ++q) v[q] = mul_f32x2(v[q], factor);
+      uint8_t* const dst = codes + 16 * i * pitch;
+      if constexpr (kFormat == LITE3R_MXFP8) {
+        uint2 w = make_uint2(e4m3x4(v[0], v[1]), e4m3x4(v[2], v[3]));
+        if (byte == 0xFFu) w = make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
+        *reinterpret_cast<uint2*>(dst) = w;
+      } else {
+        const uint32_t w = e2m1x8(v);
+        *reinterpret_cast<uint32_t*>(dst) = byte == 0xFFu ? 0x22222222u : w;
+      }
+    }
+  }
+}
 
 template <typename T, int kFormat>
 __global__ void __launch_bounds__(kMxThreads) mx_quantise_kernel(const T* __restrict__ x, long long row_stride, int rows, int cols,
@@ -110,49 +180,19 @@ __global__ void __launch_bounds__(kMxThreads) mx_quantise_kernel(const T* __rest
                                                                 uint32_t* __restrict__ scales) {
   __shared__ __align__(16) uint8_t s_scales[512];
   const int row_tile = blockIdx.x / col_tiles, col_tile = blockIdx.x - row_tile * col_tiles;
-  const int lane16 = threadIdx.x & 15, col = col_tile * kMxCols + lane16 * 8;
-  const int row_in = threadIdx.x >> 4;  // of the sixteen rows of a step
+  const int lane16 = threadIdx.x & 15, col0 = col_tile * kMxCols;
+  const int r0 = threadIdx.x >> 4;  // of the sixteen rows of a step
   const long long row0 = static_cast<long long>(row_tile) * kMxRows;
   wait_for_prior_grid();
   launch_dependents();
-  Octet<T> in[kMxIters];
-#pragma unroll
-  for (int i = 0; i < kMxIters; ++i) {
-    const long long row = row0 + row_in + 16 * i;
-    if (row < rows && col < cols) in[i].load(x + row * row_stride + col);
-    else in[i].clear();
-  }
-#pragma unroll
-  for (int i = 0; i < kMxIters; ++i) {
-    const int r = row_in + 16 * i;
-    uint32_t top = in[i].top();
-    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 1));
-    top = max(top, __shfl_xor_sync(0xFFFFFFFFu, top, 2));
-    const uint32_t byte = scale_byte<kFormat>(top);
-    if ((lane16 & 3) == 0) s_scales[(r & 31) * 16 + (r >> 5) * 4 + (lane16 >> 2)] = static_cast<uint8_t>(byte);
-    if (row0 + r < rows && col < cols) {
-      const float inverse = __uint_as_float((254u - min(byte, 253u)) << 23);
-      float v[8];
-      in[i].values(v);
-      uint8_t* dst = codes + static_cast<size_t>(row0 + r) * code_pitch<kFormat>(cols);
-      if constexpr (kFormat == LITE3R_MXFP8) {
-        uint32_t w[2];
-#pragma unroll
-        for (int q = 0; q < 2; ++q) {
-          const uint32_t lo = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * q] * inverse, v[4 * q + 1] * inverse), __NV_SATFINITE, __NV_E4M3);
-          const uint32_t hi = __nv_cvt_float2_to_fp8x2(make_float2(v[4 * q + 2] * inverse, v[4 * q + 3] * inverse), __NV_SATFINITE, __NV_E4M3);
-          w[q] = byte == 0xFFu ? 0x7F7F7F7Fu : lo | hi << 16;
-        }
-        *reinterpret_cast<uint2*>(dst + col) = make_uint2(w[0], w[1]);
-      } else {
-        uint32_t w = 0;
-#pragma unroll
-        for (int q = 0; q < 4; ++q)
-          w |= static_cast<uint32_t>(__nv_cvt_float2_to_fp4x2(make_float2(v[2 * q] * inverse, v[2 * q + 1] * inverse), __NV_E2M1, cudaRoundNearest)) << (8 * q);
-        *reinterpret_cast<uint32_t*>(dst + col / 2) = byte == 0xFFu ? 0x22222222u : w;
-      }
-    }
-  }
+  // byte of row r, block j at (r % 32) * 16 + (r / 32) * 4 + j
+  const uint32_t scales_at = smem_u32(s_scales) + r0 * 16 + (lane16 >> 2);
+  const T* const src = x + (row0 + r0) * row_stride + col0 + lane16 * 8;
+  uint8_t* const dst = codes + static_cast<size_t>(row0 + r0) * code_pitch<kFormat>(cols) + (col0 + lane16 * 8) / (kFormat == LITE3R_MXFP4 ? 2 : 1);
+  const int rows_left = static_cast<int>(min(static_cast<long long>(kMxRows), rows - row0)), cols_left = min(kMxCols, cols - col0);
+  const size_t pitch = code_pitch<kFormat>(cols);
+  if (rows_left == kMxRows && cols_left == kMxCols) quantise_tile<T, kFormat, true>(src, row_stride, rows_left, cols_left, dst, pitch, scales_at, r0, lane16);
+  else quantise_tile<T, kFormat, false>(src, row_stride, rows_left, cols_left, dst, pitch, scales_at, r0, lane16);
   __syncthreads();
   if (threadIdx.x < 128) scales[static_cast<size_t>(blockIdx.x) * 128 + threadIdx.x] = reinterpret_cast<const uint32_t*>(s_scales)[threadIdx.x];
 }
