@@ -33,7 +33,7 @@ struct Layout {
   static constexpr int kCtas = kPair ? 2 : 1;
   static constexpr int kGroups = kN / 64;                      // epilogue warpgroups
   static constexpr int kThreads = 128 + 128 * kGroups;
-  static constexpr int kStages = kPair ? 4 : 5;
+  static constexpr int kStages = 5;
   static constexpr int kLoadN = kN / kCtas;                    // rows of B that this CTA loads
   static constexpr int kTilesB = (kN + 127) / 128;             // scale tiles of B per 128 elements of K: of all columns in both CTAs
   static constexpr uint32_t kOffB = kTileM * kRowBytes;
@@ -41,8 +41,8 @@ struct Layout {
   static constexpr uint32_t kOffSfb = kOffSfa + 2 * kScaleTile;
   static constexpr uint32_t kScaleBytes = (2 + 2 * kTilesB) * kScaleTile;
   static constexpr uint32_t kStageBytes = kOffSfa + kScaleBytes;
-  static constexpr uint32_t kOffOut = kStages * kStageBytes;   // staged output, 4 KB per epilogue warp
-  static constexpr uint32_t kOffBias = kOffOut + kGroups * 16384;  // two sets by turns
+  static constexpr uint32_t kOffOut = kStages * kStageBytes;   // staged output, 2 KB per epilogue warp
+  static constexpr uint32_t kOffBias = kOffOut + kGroups * 8192;  // two sets by turns
   static constexpr uint32_t kOffBar = kOffBias + 2 * kN * 4;
   static constexpr uint32_t kSmemBytes = kOffBar + 256;
   // tensor memory: two accumulators, then the scales of a stage: four columns per scale tile
@@ -226,9 +226,9 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
     const int quarter = warp & 3;
     const int hh = (warp - 4) >> 2;  // which 64 columns of the tile this warpgroup owns
     const int tid = threadIdx.x - (4 + hh * 4) * 32;
-    uint8_t* const warp_tile = smem + L::kOffOut + hh * 16384 + quarter * 4096;
-    const uint32_t my_row = smem_u32(warp_tile) + lane * 128;
-    const int swz = lane & 7;
+    uint8_t* const warp_tile = smem + L::kOffOut + hh * 8192 + quarter * 2048;
+    const uint32_t my_row = smem_u32(warp_tile) + lane * 64;
+    const int swz = (lane >> 1) & 3;
     const bool wide = p.y_dtype == LITE3R_F32;
     bool ok = true;
     int it = 0;
@@ -248,7 +248,7 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          if constexpr (kPair) mbar_arrive_cluster(cluster_u32(bar, 0));
+          if constexpr (kPair) mbar_arrive_cluster_own(cluster_u32(bar, 0));
           else mbar_arrive(bar);
         }
       };
@@ -259,8 +259,9 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         read_out(&bars->acc_empty[ab]);
         continue;
       }
-      // The warp stages its 32 rows, 128 bytes at a time, in the layout the store engine reads (128B swizzle); rows and
-      // columns past the output are clipped by the engine, columns at 16 bytes: a ragged end is stored value by value.
+      // The warp stages its 32 rows, 64 bytes at a time (which leaves room for a fifth stage of operands), in the layout the
+      // store engine reads (64B swizzle); rows and columns past the output are clipped by the engine, columns at 16 bytes: a
+      // ragged end is stored value by value.
       const bool ragged = p.ragged && col + 64 > p.d_out;
       const int first_cb = shares && ab == 0 ? 32 : 0;
 #pragma unroll 1
@@ -268,10 +269,6 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         const int cb = j == 0 ? first_cb : 32 - first_cb;
         uint32_t v[32];
         tmem_ld32(acc_addr + cb, v);
-        if (wide || j == 0) {  // what was staged here before has been read by the store engine
-          if (lane == 0) bulk_wait_group_read0();
-          __syncwarp();
-        }
         tmem_wait_ld();
         if (shares && j == 0) read_out(&bars->shared_read);
         if (j == 1) read_out(&bars->acc_empty[ab]);
@@ -297,34 +294,39 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
           }
           continue;
         }
-        if (wide) {
+        auto store = [&](int first, const uint32_t (&w)[16]) {  // 64 bytes of the row, from this column on
+          if (lane == 0) bulk_wait_group_read0();  // what was staged here before has been read by the store engine
+          __syncwarp();
 #pragma unroll
-          for (int c = 0; c < 8; ++c) sts128(my_row + ((c ^ swz) << 4), v[4 * c], v[4 * c + 1], v[4 * c + 2], v[4 * c + 3]);
-        } else {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            uint32_t w[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-              const float y0 = __uint_as_float(v[8 * c + 2 * q]), y1 = __uint_as_float(v[8 * c + 2 * q + 1]);
-              if (p.y_dtype == LITE3R_BF16) {
-                __nv_bfloat162 h = __floats2bfloat162_rn(y0, y1);
-                w[q] = *reinterpret_cast<uint32_t*>(&h);
-              } else {
-                __half2 h = __floats2half2_rn(y0, y1);
-                w[q] = *reinterpret_cast<uint32_t*>(&h);
-              }
-            }
-            sts128(my_row + (((cb / 8 + c) ^ swz) << 4), w[0], w[1], w[2], w[3]);
-          }
-        }
-        if (wide || j == 1) {
+          for (int c = 0; c < 4; ++c) sts128(my_row + ((c ^ swz) << 4), w[4 * c], w[4 * c + 1], w[4 * c + 2], w[4 * c + 3]);
           fence_proxy_async_smem();
           __syncwarp();
           if (lane == 0) {
-            if (col + (wide ? cb : 0) < p.d_out) tma_store_2d(&map_y, warp_tile, col + (wide ? cb : 0), row0 + quarter * 32);
+            if (col + first < p.d_out) tma_store_2d(&map_y, warp_tile, col + first, row0 + quarter * 32);
             bulk_commit_group();
           }
+        };
+        uint32_t w[16];
+        if (wide) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+#pragma unroll
+            for (int c = 0; c < 16; ++c) w[c] = v[16 * h + c];
+            store(cb + 16 * h, w);
+          }
+        } else {
+#pragma unroll
+          for (int q = 0; q < 16; ++q) {
+            const float y0 = __uint_as_float(v[2 * q]), y1 = __uint_as_float(v[2 * q + 1]);
+            if (p.y_dtype == LITE3R_BF16) {
+              __nv_bfloat162 h = __floats2bfloat162_rn(y0, y1);
+              w[q] = *reinterpret_cast<uint32_t*>(&h);
+            } else {
+              __half2 h = __floats2half2_rn(y0, y1);
+              w[q] = *reinterpret_cast<uint32_t*>(&h);
+            }
+          }
+          store(cb, w);
         }
       }
     }
@@ -402,7 +404,7 @@ lite3r_status launch_linear_mxf4(const uint8_t* x_codes, const uint8_t* x_scales
                           y_dtype == LITE3R_F32    ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
                           : y_dtype == LITE3R_BF16 ? CU_TENSOR_MAP_DATA_TYPE_BFLOAT16
                                                    : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
-                          elem, y, d_out, rows, 128 / elem, 32, CU_TENSOR_MAP_SWIZZLE_128B, static_cast<uint64_t>(y_stride) * elem);
+                          elem, y, d_out, rows, 64 / elem, 32, CU_TENSOR_MAP_SWIZZLE_64B, static_cast<uint64_t>(y_stride) * elem);
   if (st != LITE3R_OK) return st;
   // Pairs on 256 x 256 from more than one such tile for every two pairs; below that more and smaller tiles use more SMs.
   const long long row_tiles = ceil_div(rows, kTileM);

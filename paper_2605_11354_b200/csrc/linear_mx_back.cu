@@ -436,7 +436,7 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster(cluster_u32(&bars->acc_empty[ab], 0));
+        if (lane == 0) mbar_arrive_cluster_own(cluster_u32(&bars->acc_empty[ab], 0));
       }
     }
     bulk_wait_group_read0();  // what is staged stays in place until it has been read

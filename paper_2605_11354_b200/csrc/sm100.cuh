@@ -385,9 +385,9 @@ __device__ __forceinline__ uint32_t cluster_u32(const void* p, uint32_t rank) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
-// The same after writes to this CTA's own shared memory that a product of the pair will read from there: their order need only
-// hold where they are, in this CTA (a release at cluster scope waits until everything is performed for the whole GPU: 1800
-// cycles in the converting warps of the backward GEMM).
+// The same after writes to this CTA's own shared memory that a product of the pair will read from there, or reads of its own
+// tensor memory that one will write: their order need only hold where they are, in this CTA (a release at cluster scope waits
+// until everything is performed for the whole GPU: 1800 cycles in the converting warps of the backward GEMM).
 __device__ __forceinline__ void mbar_arrive_cluster_own(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
