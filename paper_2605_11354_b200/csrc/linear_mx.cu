@@ -128,27 +128,30 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
   launch_dependents();
   if (blockIdx.x == 0 && threadIdx.x == 0 && p.status != nullptr) *p.status = 0;
 
+  // The loops of the loading and issuing warps run in all lanes and one of them issues: addresses and descriptors then stay in
+  // uniform registers (in a loop of one lane a load took 200 cycles to issue, and 40 idle cycles lay between two products of 128).
   if (warp == 0 || warp == 2) {
-    if (lane == 0) {
-      const bool operands = warp == 0;
+    const bool operands = warp == 0, issuer = elect_one();
+    if (issuer) {
       tma_prefetch_desc(operands ? &map_x : &map_xs);
       tma_prefetch_desc(operands ? &map_w : &map_ws);
-      constexpr uint32_t kOperandBytes = L::kOffSfa;
-      bool ok = true;
-      int kc = 0;
-      for (int tile = first_tile; ok && tile < p.tiles; tile += tile_step) {
-        const int row_tile = tile / p.col_tiles, col0 = (tile - row_tile * p.col_tiles) * kN;
-        const int row0 = (row_tile * kCtas + rank) * kTileM;
-        for (int k = 0; ok && k < stages_k; ++k, ++kc) {
-          const int st = kc % kStages;
-          if (kc >= kStages)
-            ok = mbar_wait_clearing(&bars->empty[st], ((kc - kStages) / kStages) & 1, abort_flag, p.status, 801);
-          if (!ok) break;
+    }
+    constexpr uint32_t kOperandBytes = L::kOffSfa;
+    const uint32_t full0 = kPair ? cluster_u32(&bars->full[0], 0) : 0u;  // both CTAs' loads count on the first one's barrier
+    bool ok = true;
+    int kc = 0, st = 0;
+    uint32_t parity = 1;  // of the stage's use before, from the second round on
+    for (int tile = first_tile; ok && tile < p.tiles; tile += tile_step) {
+      const int row_tile = tile / p.col_tiles, col0 = (tile - row_tile * p.col_tiles) * kN;
+      const int row0 = (row_tile * kCtas + rank) * kTileM;
+      for (int k = 0; ok && k < stages_k; ++k, ++kc) {
+        if (kc >= kStages) ok = mbar_wait_clearing(&bars->empty[st], parity, abort_flag, p.status, 801);
+        if (!ok) break;
+        if (issuer) {
           uint8_t* const dst = smem + st * L::kStageBytes;
-          // both CTAs' loads count on the first one's barrier
           if (rank == 0) mbar_arrive_expect_tx(&bars->full[st], kCtas * (operands ? kOperandBytes : L::kScaleBytes));
           auto load = [&](uint32_t off, const CUtensorMap* map, int x, int y) {
-            if constexpr (kPair) tma_load_2d_pair(dst + off, map, cluster_u32(&bars->full[st], 0), x, y);
+            if constexpr (kPair) tma_load_2d_pair(dst + off, map, full0 + st * 8, x, y);
             else tma_load_2d(dst + off, map, &bars->full[st], x, y);
           };
           if (operands) {
@@ -161,11 +164,13 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
               load(L::kOffSfb + b * 2 * kScaleTile, &map_ws, 0, (col0 / 128 + b) * p.k_tiles + 2 * k);
           }
         }
+        if (++st == kStages) {
+          st = 0;
+          parity ^= 1u;
+        }
       }
     }
   } else if (warp == 1) {
-    // The loop runs in all lanes and one of them issues: descriptors then stay in uniform registers (worked out by one lane
-    // they left 40 idle cycles between two products of 128).
     if (rank == 0) {
       const bool issuer = elect_one();
       constexpr uint32_t idesc0 = instr_desc_mxf4(kCtas * kTileM, kN, 0), idesc2 = instr_desc_mxf4(kCtas * kTileM, kN, 2);
@@ -174,7 +179,8 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
       const uint64_t s_desc0 = smem_desc(smem_u32(smem) + L::kOffSfa, 16, 128, 0);
       const int products = (p.d_in + 63) / 64;
       bool ok = true;
-      int kc = 0, it = 0;
+      int st = 0, it = 0;
+      uint32_t parity = 0;
       for (int tile = first_tile; ok && tile < p.tiles; tile += tile_step, ++it) {
         const int ab = it & 1;
         const uint32_t acc = tmem + (ab ? L::kAcc1 : 0u);
@@ -183,9 +189,8 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         if (it >= 2) ok = mbar_wait_clearing(&bars->acc_empty[ab], ((it - 2) >> 1) & 1, abort_flag, p.status, 804);
         if (L::kShared != 0 && ok && it >= 1) ok = mbar_wait_clearing(&bars->shared_read, (it - 1) & 1, abort_flag, p.status, 805);
         tc_fence_after();
-        for (int k = 0; ok && k < stages_k; ++k, ++kc) {
-          const int st = kc % kStages;
-          ok = mbar_wait_clearing(&bars->full[st], (kc / kStages) & 1, abort_flag, p.status, 802);
+        for (int k = 0; ok && k < stages_k; ++k) {
+          ok = mbar_wait_clearing(&bars->full[st], parity, abort_flag, p.status, 802);
           if (!ok) break;
           tc_fence_after();
           const uint64_t off = static_cast<uint64_t>((st * L::kStageBytes) >> 4);
@@ -214,6 +219,10 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
             }
             if constexpr (kPair) mma_commit_pair(&bars->empty[st]);
             else mma_commit(&bars->empty[st]);
+          }
+          if (++st == kStages) {
+            st = 0;
+            parity ^= 1u;
           }
         }
         if (ok && issuer) {
