@@ -198,42 +198,50 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
   };
   const int first_unit = blockIdx.x >> 1, unit_step = gridDim.x >> 1;
 
+  // The loops of the loading and issuing warps run in all lanes and one of them issues: addresses and descriptors then stay in
+  // uniform registers (in a loop of one lane a load took 200 cycles to issue, and 40 idle cycles lay between two products of 128).
   if (warp == 0) {
-    if (lane == 0) {
-      tma_prefetch_desc(&map_codes);
-      bool ok = true;
-      int kc = 0;
-      for (int unit = first_unit; ok && unit < p.units; unit += unit_step) {
-        const UnitAt u = unit_at(unit);
-        const int n = u.n0 + rank * (u.half ? 64 : 128);  // this CTA's columns
-        const bool scales = n / 128 < p.scale_tiles;      // (none where they are all past the end)
-        const uint32_t bytes = (u.half ? 1 : 2) * kTileR * L::kBoxBytes + (scales ? kScaleTile : 0);
-        for (int k = u.first; ok && k < u.last; ++k, ++kc) {
-          const int st = kc % kRaw;
-          if (kc >= kRaw) ok = mbar_wait_clearing(&bars->raw_empty[st], ((kc - kRaw) / kRaw) & 1, abort_flag, p.status, 811, 32);
-          if (!ok) break;
+    const bool issuer = elect_one();
+    if (issuer) tma_prefetch_desc(&map_codes);
+    bool ok = true;
+    int kc = 0, st = 0;
+    uint32_t parity = 1;  // of the stage's use before, from the second round on
+    for (int unit = first_unit; ok && unit < p.units; unit += unit_step) {
+      const UnitAt u = unit_at(unit);
+      const int n = u.n0 + rank * (u.half ? 64 : 128);  // this CTA's columns
+      const bool scales = n / 128 < p.scale_tiles;      // (none where they are all past the end)
+      const uint32_t bytes = (u.half ? 1 : 2) * kTileR * L::kBoxBytes + (scales ? kScaleTile : 0);
+      const int x = kFormat == LITE3R_MXFP8 ? n : n / 2;
+      for (int k = u.first; ok && k < u.last; ++k, ++kc) {
+        if (kc >= kRaw) ok = mbar_wait_clearing(&bars->raw_empty[st], parity, abort_flag, p.status, 811);
+        if (!ok) break;
+        if (issuer) {
           uint8_t* const dst = smem + L::kOffRaw + st * L::kRawBytes;
           mbar_arrive_expect_tx(&bars->raw_full[st], bytes);
-          const int x = kFormat == LITE3R_MXFP8 ? n : n / 2;
           tma_load_2d(dst, &map_codes, &bars->raw_full[st], x, k * kTileR);
           if (!u.half) tma_load_2d(dst + kTileR * L::kBoxBytes, &map_codes, &bars->raw_full[st], x + L::kBoxBytes, k * kTileR);
           if (scales)
             bulk_load(dst + L::kOffScales, p.scales + (static_cast<size_t>(k / 2) * p.scale_tiles + n / 128) * kScaleTile, kScaleTile,
                       &bars->raw_full[st]);
         }
+        if (++st == kRaw) {
+          st = 0;
+          parity ^= 1u;
+        }
       }
     }
   } else if (warp == 2) {
-    if (lane == 0) {
-      tma_prefetch_desc(&map_dy);
-      bool ok = true;
-      int kc = 0;
-      for (int unit = first_unit; ok && unit < p.units; unit += unit_step) {
-        const UnitAt u = unit_at(unit);
-        for (int k = u.first; ok && k < u.last; ++k, ++kc) {
-          const int st = kc % kOps;
-          if (kc >= kOps) ok = mbar_wait_clearing(&bars->op_empty[st], ((kc - kOps) / kOps) & 1, abort_flag, p.status, 812, 32);
-          if (!ok) break;
+    const bool issuer = elect_one();
+    if (issuer) tma_prefetch_desc(&map_dy);
+    bool ok = true;
+    int kc = 0, st = 0;
+    uint32_t parity = 1;
+    for (int unit = first_unit; ok && unit < p.units; unit += unit_step) {
+      const UnitAt u = unit_at(unit);
+      for (int k = u.first; ok && k < u.last; ++k, ++kc) {
+        if (kc >= kOps) ok = mbar_wait_clearing(&bars->op_empty[st], parity, abort_flag, p.status, 812);
+        if (!ok) break;
+        if (issuer) {
           uint8_t* const dst = smem + st * L::kOpBytes;
           mbar_arrive_expect_tx(&bars->a_full[st], 128 * kTileR * 2);
           if constexpr (kWgrad) {  // two boxes of 64 columns x 64 rows of dy
@@ -243,11 +251,13 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
             tma_load_2d(dst, &map_dy, &bars->a_full[st], k * kTileR, u.m0);
           }
         }
+        if (++st == kOps) {
+          st = 0;
+          parity ^= 1u;
+        }
       }
     }
   } else if (warp == 1) {
-    // The loop runs in all lanes and one of them issues: descriptors then stay in uniform registers (worked out by one lane
-    // they left 40 idle cycles between two products of 128).
     if (rank == 0) {
       const bool issuer = elect_one();
       constexpr uint32_t idesc_wide = instr_desc(1, kTileM, kTileN, kWgrad ? 1 : 0, 1);
@@ -255,7 +265,8 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
       const uint64_t a_desc0 = kWgrad ? smem_desc(smem_u32(smem), 8192, 1024, kSwizzle128) : smem_desc(smem_u32(smem), 16, 1024, kSwizzle128);
       const uint64_t b_desc0 = smem_desc(smem_u32(smem) + L::kOffB, 8192, 1024, kSwizzle128);
       bool ok = true;
-      int kc = 0, it = 0;
+      int st = 0, it = 0;
+      uint32_t parity = 0;
       for (int unit = first_unit; ok && unit < p.units; unit += unit_step) {
         const UnitAt u = unit_at(unit);
         const uint32_t idesc = u.half ? idesc_half : idesc_wide;
@@ -263,9 +274,8 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
           const int ab = it & 1, k1 = min(k0 + p.steps_per_sum, u.last);
           if (it >= 2) ok = mbar_wait_clearing(&bars->acc_empty[ab], ((it - 2) >> 1) & 1, abort_flag, p.status, 814);
           tc_fence_after();
-          for (int k = k0; ok && k < k1; ++k, ++kc) {
-            const int st = kc % kOps;
-            ok = mbar_wait_cluster_clearing(&bars->b_full[st], (kc / kOps) & 1, abort_flag, p.status, 816);
+          for (int k = k0; ok && k < k1; ++k) {
+            ok = mbar_wait_cluster_clearing(&bars->b_full[st], parity, abort_flag, p.status, 816);
             if (!ok) break;
             tc_fence_after();
             if (issuer) {
@@ -275,6 +285,10 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
                 mma_f16_pair(tmem + ab * kTileN, a_desc0 + off + kk * ((kWgrad ? 2048 : 32) >> 4), b_desc0 + off + kk * (2048 >> 4), idesc,
                              (k > k0 || kk > 0) ? 1u : 0u);
               mma_commit_pair(&bars->op_empty[st]);
+            }
+            if (++st == kOps) {
+              st = 0;
+              parity ^= 1u;
             }
           }
           if (ok && issuer) mma_commit_pair(&bars->acc_full[ab]);
