@@ -607,10 +607,14 @@ def lite3r_mx_sizes(format: str, rows: int, cols: int):
 
 
 def alloc_mx(rows: int, cols: int, format: str, device) -> MxTensor:
+    """Buffers of a microscaled matrix, both in one piece of memory (a second allocation costs as much as the launch)."""
     if format not in MX_FORMATS or rows <= 0 or cols <= 0 or cols % 32:
         lite3r_mx_sizes(format, rows, cols)  # refuses what has no such form
-    return MxTensor(torch.empty((rows, cols if format == "mxfp8" else cols // 2), dtype=torch.uint8, device=device),
-                    torch.empty((-(-rows // 128), -(-cols // 128), 32, 4, 4), dtype=torch.uint8, device=device), rows, cols, format)
+    row_tiles, col_tiles, pitch = -(-rows // 128), -(-cols // 128), cols if format == "mxfp8" else cols // 2
+    scales = row_tiles * col_tiles * 512
+    both = torch.empty(scales + rows * pitch, dtype=torch.uint8, device=device)
+    return MxTensor(both.as_strided((rows, pitch), (pitch, 1), scales),
+                    both.as_strided((row_tiles, col_tiles, 32, 4, 4), (col_tiles * 512, 512, 16, 4, 1)), rows, cols, format)
 
 
 def _matrix(x, what: str, dtypes=OUT_DTYPES) -> int:
@@ -626,18 +630,19 @@ def lite3r_quantize_mx(x: torch.Tensor, format: str = "mxfp4", out=None, stream=
     what = "lite3r_quantize_mx"
     dtype = _matrix(x, what)
     rows, cols = x.shape
-    _on_current_device(what, x)
     if out is None:
+        _on_current_device(what, x)
         if stream is None:
             out = alloc_mx(rows, cols, format, x.device)
         else:
             with torch.cuda.stream(stream):  # memory that belongs to the stream that fills it
                 out = alloc_mx(rows, cols, format, x.device)
-    elif (out.rows, out.cols, out.format) != (rows, cols, format):
-        raise Lite3rError(f"{what}: out has another shape or format")
-    code = out.check(what)
-    _on_current_device(what, out.codes, out.scales)
-    _check(lib().lite3r_quantize_mx(x.data_ptr(), dtype, x.stride(0), rows, cols, code, out.codes.data_ptr(),
+    else:
+        if (out.rows, out.cols, out.format) != (rows, cols, format):
+            raise Lite3rError(f"{what}: out has another shape or format")
+        out.check(what)
+        _on_current_device(what, x, out.codes, out.scales)
+    _check(lib().lite3r_quantize_mx(x.data_ptr(), dtype, x.stride(0), rows, cols, MX_FORMATS[format], out.codes.data_ptr(),
                                     out.scales.data_ptr(), _stream_ptr(stream)), what)
     return out
 
