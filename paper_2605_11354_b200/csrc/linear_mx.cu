@@ -146,6 +146,7 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
       const int row0 = (row_tile * kCtas + rank) * kTileM;
       for (int k = 0; ok && k < stages_k; ++k, ++kc) {
         if (kc >= kStages) ok = mbar_wait_clearing(&bars->empty[st], parity, abort_flag, p.status, 801);
+        ok = __all_sync(0xFFFFFFFFu, ok);  // no lane falls behind by a phase
         if (!ok) break;
         if (issuer) {
           uint8_t* const dst = smem + st * L::kStageBytes;
@@ -188,9 +189,11 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         const uint32_t sfb_shift = kN == 64 ? 2u * ((tile % p.col_tiles) & 1) : 0u;
         if (it >= 2) ok = mbar_wait_clearing(&bars->acc_empty[ab], ((it - 2) >> 1) & 1, abort_flag, p.status, 804);
         if (L::kShared != 0 && ok && it >= 1) ok = mbar_wait_clearing(&bars->shared_read, (it - 1) & 1, abort_flag, p.status, 805);
+        ok = __all_sync(0xFFFFFFFFu, ok);
         tc_fence_after();
         for (int k = 0; ok && k < stages_k; ++k) {
           ok = mbar_wait_clearing(&bars->full[st], parity, abort_flag, p.status, 802);
+          ok = __all_sync(0xFFFFFFFFu, ok);
           if (!ok) break;
           tc_fence_after();
           const uint64_t off = static_cast<uint64_t>((st * L::kStageBytes) >> 4);

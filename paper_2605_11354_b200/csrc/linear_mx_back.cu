@@ -38,7 +38,11 @@ constexpr uint32_t kTmemCols = 512;
 
 template <int kFormat>
 struct Layout {
-  static constexpr int kRaw = 5, kOps = 5;                      // stages of codes, stages of operands
+  // Stages of codes, one to a group: a group that waits for its next step's codes has read the stage's last ones itself.  (With a
+  // stage more the stages pass from group to group, and a group could wait on a barrier whose phase before was still open,
+  // which a parity test takes for done.)
+  static constexpr int kRaw = kGroups;
+  static constexpr int kOps = 5;                                // stages of operands
   static constexpr int kBoxBytes = kFormat == LITE3R_MXFP8 ? 64 : 32;  // of 64 columns of codes
   static constexpr uint32_t kOffB = 128 * kTileR * 2;           // A, then B as two boxes of 64 columns x 64 rows
   static constexpr uint32_t kOpBytes = kOffB + 128 * kTileR * 2;
@@ -52,7 +56,7 @@ struct Layout {
 };
 
 struct Bars {
-  uint64_t raw_full[5], raw_empty[5], a_full[5], op_empty[5];
+  uint64_t raw_full[kGroups], raw_empty[kGroups], a_full[5], op_empty[5];
   uint64_t b_full[5];                   // of the first CTA: both CTAs' operands are there
   uint64_t acc_full[2], acc_empty[2];   // acc_empty: of the first CTA
   uint32_t tmem_base;
@@ -214,6 +218,7 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
       const int x = kFormat == LITE3R_MXFP8 ? n : n / 2;
       for (int k = u.first; ok && k < u.last; ++k, ++kc) {
         if (kc >= kRaw) ok = mbar_wait_clearing(&bars->raw_empty[st], parity, abort_flag, p.status, 811);
+        ok = __all_sync(0xFFFFFFFFu, ok);  // no lane falls behind by a phase
         if (!ok) break;
         if (issuer) {
           uint8_t* const dst = smem + L::kOffRaw + st * L::kRawBytes;
@@ -240,6 +245,7 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
       const UnitAt u = unit_at(unit);
       for (int k = u.first; ok && k < u.last; ++k, ++kc) {
         if (kc >= kOps) ok = mbar_wait_clearing(&bars->op_empty[st], parity, abort_flag, p.status, 812);
+        ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
         if (issuer) {
           uint8_t* const dst = smem + st * L::kOpBytes;
@@ -273,9 +279,11 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
         for (int k0 = u.first; ok && k0 < u.last; k0 += p.steps_per_sum, ++it) {
           const int ab = it & 1, k1 = min(k0 + p.steps_per_sum, u.last);
           if (it >= 2) ok = mbar_wait_clearing(&bars->acc_empty[ab], ((it - 2) >> 1) & 1, abort_flag, p.status, 814);
+          ok = __all_sync(0xFFFFFFFFu, ok);
           tc_fence_after();
           for (int k = k0; ok && k < k1; ++k) {
             ok = mbar_wait_cluster_clearing(&bars->b_full[st], parity, abort_flag, p.status, 816);
+            ok = __all_sync(0xFFFFFFFFu, ok);
             if (!ok) break;
             tc_fence_after();
             if (issuer) {
@@ -313,9 +321,8 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
       const int mine = (group - kc % kGroups + kGroups) % kGroups;  // the first step of the unit that is this group's
       for (int i = mine; ok && i < steps; i += kGroups) {
         const int at = kc + i, k = u.first + i;
-        const int rs = at % kRaw, st = at % kOps;
+        const int rs = group, st = at % kOps;
         ok = mbar_wait_clearing(&bars->raw_full[rs], (at / kRaw) & 1, abort_flag, p.status, 817);
-        if (ok && at >= kOps) ok = mbar_wait_clearing(&bars->op_empty[st], ((at - kOps) / kOps) & 1, abort_flag, p.status, 818);
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;
         const uint32_t raw = my_raw + rs * L::kRawBytes, dst = my_b + st * L::kOpBytes;
@@ -331,6 +338,11 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
           c[q].load(raw + q * (32 * L::kBoxBytes));
           if (!u.half) c[2 + q].load(raw + (kTileR + 32 * q) * L::kBoxBytes);
         }
+        __syncwarp();
+        if (lane == 0) mbar_arrive(&bars->raw_empty[rs]);  // codes and scales are in registers
+        if (at >= kOps) ok = mbar_wait_clearing(&bars->op_empty[st], ((at - kOps) / kOps) & 1, abort_flag, p.status, 818);
+        ok = __all_sync(0xFFFFFFFFu, ok);
+        if (!ok) break;
         auto convert = [&](auto far) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
@@ -365,10 +377,7 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
           }
         }
         __syncwarp();
-        if (lane == 0) {
-          mbar_arrive_cluster_own(cluster_u32(&bars->b_full[st], 0));
-          mbar_arrive(&bars->raw_empty[rs]);
-        }
+        if (lane == 0) mbar_arrive_cluster_own(cluster_u32(&bars->b_full[st], 0));
       }
       kc += steps;
       if (sums && ok && mine < steps) {
