@@ -418,10 +418,14 @@ lite3r_status launch_linear_mxf4(const uint8_t* x_codes, const uint8_t* x_scales
                                                    : CU_TENSOR_MAP_DATA_TYPE_FLOAT16,
                           elem, y, d_out, rows, 64 / elem, 32, CU_TENSOR_MAP_SWIZZLE_64B, static_cast<uint64_t>(y_stride) * elem);
   if (st != LITE3R_OK) return st;
-  // Pairs on 256 x 256 from more than one such tile for every two pairs; below that more and smaller tiles use more SMs.
+  // Tiles of 64 columns while they are at most one to an SM, then of 128 until there are more tiles of 256 x 256 than pairs, or
+  // half as many where the contraction is long.  us with tiles of 64 / 128 / 256 columns (rows x d_in x d_out):
+  //   777 x 1024 x 1024  4.0 / 4.5 / 5.7    1374 x 4096 x 1024  10.3 / 7.5 / 9.3    2748 x 1024 x 1024   6.4 /  5.9 /  6.4
+  //   2748 x 4096 x 1024  14.4 / 10.9 / 10.0    10992 x 1024 x 4096  48.1 / 31.6 / 26.2
   const long long row_tiles = ceil_div(rows, kTileM);
-  if (static_cast<long long>(ceil_div(d_out, 256)) * ceil_div(rows, 256) > sms / 4) return launch_tiles<256>(o, map_y, p, sms, stream);
-  return ceil_div(d_out, 128) * row_tiles < sms ? launch_tiles<64>(o, map_y, p, sms, stream) : launch_tiles<128>(o, map_y, p, sms, stream);
+  const long long large = static_cast<long long>(ceil_div(d_out, 256)) * ceil_div(rows, 256);
+  if (large * (d_in >= 2048 ? 2 : 1) > sms / 2) return launch_tiles<256>(o, map_y, p, sms, stream);
+  return ceil_div(d_out, 64) * row_tiles <= sms ? launch_tiles<64>(o, map_y, p, sms, stream) : launch_tiles<128>(o, map_y, p, sms, stream);
 }
 
 }  // namespace lite3r

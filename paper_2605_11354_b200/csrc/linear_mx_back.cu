@@ -518,15 +518,17 @@ constexpr int kBiasCols = 4;
 constexpr int kMostPairs = 128;  // of any device, for the size of the workspace
 
 // How the tiles are cut.  Columns: all of 256, or the last 256 in two halves, which run last and fill the gaps that whole tiles
-// leave (10992 x 1024: 172 tiles on 74 pairs take three rounds, 129 and 86 halves two and a half), or halves throughout
-// (few tiles).
+// leave, or halves throughout (few tiles).  A step of a half tile takes three quarters of a whole one's time (0.34 and 0.45 us:
+// its conversion chain and its loads of A are as long).  dgrad of 10992 rows, 1024 x 1024: 22.4 us with 129 whole tiles and 86
+// halves, 24.3 with 172 whole ones, 31.1 with halves; 777 rows: 11.7 with whole tiles, 9.4 with halves.
 struct Cut {
   int wide, half, row_tiles, parts;
 };
-// Time in halves: a pair takes units p, p + pairs, ..., whole tiles first, so pair 0 has most of both.
+// Time in quarters of a whole tile's: a pair takes units p, p + pairs, ..., whole tiles first, so pair 0 has most of both.
 long long most_columns(const Cut& c, int pairs) {
   const long long wide = static_cast<long long>(c.wide) * c.row_tiles * c.parts, all = wide + static_cast<long long>(c.half) * c.row_tiles * c.parts;
-  return (wide + pairs - 1) / pairs + (all + pairs - 1) / pairs;
+  const long long whole = (wide + pairs - 1) / pairs, rounds = (all + pairs - 1) / pairs;
+  return 4 * whole + 3 * (rounds - whole);
 }
 Cut cut_tiles(int m_total, int n_total, int parts, int pairs) {
   const int n = ceil_div(n_total, kTileN / 2), rows = ceil_div(m_total, kTileM);  // halves per row of tiles
@@ -536,7 +538,7 @@ Cut cut_tiles(int m_total, int n_total, int parts, int pairs) {
     if (half > n) continue;
     const Cut c = {(n - half) / 2, half, rows, parts};
     const long long time = most_columns(c, pairs);
-    if (time * 16 < least * 15) {  // (halves read A twice as often)
+    if (time < least) {
       best = c;
       least = time;
     }
@@ -544,19 +546,20 @@ Cut cut_tiles(int m_total, int n_total, int parts, int pairs) {
   return best;
 }
 
-// Parts of the contraction of wgrad: the number with the least time, in steps of a half tile, of the products (a part's steps
-// and four to fill and drain the pipeline) and of writing and reading its partial results, 8 bytes per value and part at about
-// 4 TB/s against 0.15 us a step.
+// Parts of the contraction of wgrad: the number with the least time, of the products (0.113 us for a quarter of a whole tile's
+// step; four steps to fill and drain the pipeline) and of the partial results (1.5 us for the kernel that adds them; they are
+// written and read at about 10 TB/s, mostly in L2).  10992 rows, 1024 x 1024: 60 us in one part, 36 in two, 28 in four.
 int wgrad_parts(int rows, int d_in, int d_out, int pairs) {
   const int steps = ceil_div(rows, kTileR);
-  const double add = static_cast<double>(d_in) * d_out * 8.0 / 4e6 / 0.15;
+  const double megabytes = static_cast<double>(d_in) * d_out * 4e-6;
   int best = 1;
   double least = 1e300;
   for (int parts = 1; parts <= std::max(1, std::min(16, steps / 8)); ++parts) {
     const int per_part = ceil_div(steps, parts);
     if (ceil_div(steps, per_part) != parts) continue;  // none is empty
-    const double time = static_cast<double>(most_columns(cut_tiles(d_out, d_in, parts, pairs), pairs)) * (per_part + 4) + (parts > 1 ? add * parts + 20 : 0);
-    if (time < least * 0.97) {
+    const double time = 0.113 * static_cast<double>(most_columns(cut_tiles(d_out, d_in, parts, pairs), pairs)) * (per_part + 4) +
+                        (parts > 1 ? 1.5 + 0.1 * megabytes * (2 * parts + 1) : 0.0);
+    if (time < least) {
       best = parts;
       least = time;
     }
