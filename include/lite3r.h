@@ -288,7 +288,7 @@ typedef struct {
   int axes;                                            /* 0: no rotation; 1: along the sequence; 2: row and column */
   const int* positions; /* DEVICE int32 [batch][tokens][axes] (not read when axes is 0), of any sign; strides in elements, */
   long long position_stride_b, position_stride_n; /* stride 0 for positions that sequences (or tokens) share */
-  double base;                                    /* > 0 */
+  double base;                                    /* between 1e-30 and 1e30 */
 } lite3r_rope;
 
 /* Queries and keys of one attention call in one launch.  q, k: DEVICE [batch, heads, tokens, head_dim] in fp32, bf16 or fp16 with
@@ -313,7 +313,8 @@ typedef struct {
  * q, k: the sources of the forward (before the norm); dq_out, dk_out: the gradients of its results; dq, dk: written, one row
  * for every row of q and k also where the sources are broadcast.  All tensors as in the forward; dq may take the place of q or
  * of dq_out, dk that of k or dk_out.  Sums are fp32 in a fixed order.  workspace: DEVICE, 256-byte aligned,
- * lite3r_qk_norm_rope_workspace() bytes. */
+ * lite3r_qk_norm_rope_workspace() bytes; its contents are scratch, and calls (or captured graphs) that may overlap on the GPU
+ * need one each. */
 LITE3R_API lite3r_status lite3r_qk_norm_rope_backward(const lite3r_tensor* q, const lite3r_tensor* k, const lite3r_tensor* dq_out,
                                            const lite3r_tensor* dk_out, const lite3r_rope* how, const lite3r_tensor* dq,
                                            const lite3r_tensor* dk, const lite3r_rope_grads* grads, void* workspace,
@@ -356,6 +357,9 @@ LITE3R_API lite3r_status lite3r_linear_mxfp4(const unsigned char* x_codes, const
 /* Bytes of scratch of lite3r_linear_mx_wgrad.  Host-only. */
 LITE3R_API lite3r_status lite3r_linear_mx_workspace(int rows, int d_in, int d_out, size_t* bytes);
 
+/* (The codes and scales of the calls below are those that lite3r_quantize_mx writes: scales past the matrix are zero, and an
+ * e4m3 NaN stands under a NaN scale only.) */
+
 /* Gradient of a linear layer's input through its quantised weight (the quantisers pass gradients straight through):
  * dx = dy . Q(W), bf16 x codes (which become bf16 exactly) with fp32 accumulation.  dy: DEVICE bf16 [rows, d_out], row pitch
  * dy_stride elements (a multiple of 8), 16-byte aligned; w_codes, w_scales: [d_out, d_in] in `format`; dx: DEVICE [rows, d_in]
@@ -367,7 +371,8 @@ LITE3R_API lite3r_status lite3r_linear_mx_dgrad(const void* dy, long long dy_str
 /* Gradient of a linear layer's weight and bias from the kept form of its input: dw = dy^T . C(x), db = sum of dy over the rows.
  * dy as above; x_codes, x_scales: [rows, d_in] in `format` (MXFP8 for activations that were kept for this); dw: DEVICE fp32
  * [d_out, d_in], 16-byte aligned; db: DEVICE fp32 [d_out] or NULL.  Partial sums over the rows are added in a fixed order.
- * workspace: DEVICE, 256-byte aligned, lite3r_linear_mx_workspace() bytes. */
+ * workspace: DEVICE, 256-byte aligned, lite3r_linear_mx_workspace() bytes; its contents are scratch, and calls (or captured
+ * graphs) that may overlap on the GPU need one each. */
 LITE3R_API lite3r_status lite3r_linear_mx_wgrad(const void* dy, long long dy_stride, const unsigned char* x_codes,
                                      const unsigned char* x_scales, lite3r_mx_format format, int rows, int d_in, int d_out,
                                      float* dw, float* db, void* workspace, size_t workspace_bytes, int* device_status,

@@ -489,6 +489,14 @@ def _rows_of_heads(x, dtype, shape, what: str) -> bytes:
     return TENSOR.pack(x.data_ptr(), OUT_DTYPES[dtype], b, h, n)
 
 
+def _status_ptr(x, what: str):
+    if x is None:
+        return None
+    if x.dtype != torch.int32 or x.numel() < 1:
+        raise Lite3rError(f"{what}: device_status must be an int32 tensor")
+    return x.data_ptr()
+
+
 def _vector(x, dim: int, what: str) -> int:
     if x is None:
         return 0
@@ -670,7 +678,7 @@ def lite3r_linear_mxfp4(x: MxTensor, w: MxTensor, bias, y: torch.Tensor, device_
         raise Lite3rError(f"{what}: y must be [{x.rows}, {w.rows}]")
     _check(lib().lite3r_linear_mxfp4(x.codes.data_ptr(), x.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(),
                                      _vector(bias, w.rows, what), x.rows, x.cols, w.rows, y.data_ptr(), dtype, y.stride(0),
-                                     device_status.data_ptr() if device_status is not None else None, _stream_ptr(stream)), what)
+                                     _status_ptr(device_status, what), _stream_ptr(stream)), what)
 
 
 def lite3r_linear_mx_workspace(rows: int, d_in: int, d_out: int) -> int:
@@ -690,7 +698,7 @@ def lite3r_linear_mx_dgrad(dy: torch.Tensor, w: MxTensor, dx: torch.Tensor, devi
         raise Lite3rError(f"{what}: dy must be [rows, {w.rows}] and dx [rows, {w.cols}]")
     _check(lib().lite3r_linear_mx_dgrad(dy.data_ptr(), dy.stride(0), w.codes.data_ptr(), w.scales.data_ptr(), code, dy.shape[0],
                                         w.cols, w.rows, dx.data_ptr(), dtype, dx.stride(0),
-                                        device_status.data_ptr() if device_status is not None else None, _stream_ptr(stream)), what)
+                                        _status_ptr(device_status, what), _stream_ptr(stream)), what)
 
 
 def lite3r_linear_mx_wgrad(dy: torch.Tensor, x: MxTensor, dw: torch.Tensor, db, workspace: torch.Tensor, device_status=None,
@@ -705,7 +713,7 @@ def lite3r_linear_mx_wgrad(dy: torch.Tensor, x: MxTensor, dw: torch.Tensor, db, 
         raise Lite3rError(f"{what}: dy must be [{x.rows}, d_out] and dw contiguous float32 [d_out, {x.cols}]")
     _check(lib().lite3r_linear_mx_wgrad(dy.data_ptr(), dy.stride(0), x.codes.data_ptr(), x.scales.data_ptr(), code, x.rows, x.cols,
                                         dy.shape[1], dw.data_ptr(), _vector(db, dy.shape[1], what), workspace.data_ptr(),
-                                        _bytes_of(workspace, what), device_status.data_ptr() if device_status is not None else None,
+                                        _bytes_of(workspace, what), _status_ptr(device_status, what),
                                         _stream_ptr(stream)), what)
 
 

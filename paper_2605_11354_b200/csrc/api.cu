@@ -626,7 +626,7 @@ static lite3r_status check_rope(const lite3r_rope* how) {
   if (how->axes > 0) {
     if (how->positions == nullptr || !aligned(how->positions, 4) || how->position_stride_b < 0 || how->position_stride_n < 0)
       return LITE3R_ERR_INVALID_ARG;
-    if (!(how->base > 0.0) || std::isinf(how->base)) return LITE3R_ERR_INVALID_ARG;
+    if (!(how->base >= 1e-30 && how->base <= 1e30)) return LITE3R_ERR_INVALID_ARG;
   }
   return LITE3R_OK;
 }

@@ -142,6 +142,7 @@ def grads(q_weight=None, q_bias=None, k_weight=None, k_bias=None):
     (dict(axes=-1), UNSUPPORTED), (dict(eps=-1.0), INVALID), (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID),
     (dict(positions=None), INVALID), (dict(positions=P + 2), INVALID), (dict(position_stride_n=-2), INVALID),
     (dict(base=0.0), INVALID), (dict(base=float("nan")), INVALID), (dict(base=float("inf")), INVALID),
+    (dict(base=-5.0), INVALID), (dict(base=1e-31), INVALID), (dict(base=1e31), INVALID),
     (dict(q_weight=P + 4), INVALID), (dict(k_bias=P + 8), INVALID)])
 def test_rope_refuses_settings(library, change, status):
     s = source()
