@@ -480,13 +480,13 @@ def _bytes_of(workspace, what: str) -> int:
 
 def _rows_of_heads(x, dtype, shape, what: str) -> bytes:
     """lite3r_tensor of a [B,H,N,D] tensor that has to be of this dtype and shape."""
-    b, h, n, d = x.stride() if x.dim() == 4 else (0, 0, 0, 0)
-    if d != 1:
+    stride = x.stride()
+    if len(stride) != 4 or stride[3] != 1:
         raise Lite3rError(f"{what}: q, k and their results must be [B,H,N,D] with contiguous D")
-    if x.dtype != dtype or x.shape != shape:
+    if x.dtype is not dtype or x.shape != shape:
         raise Lite3rError(f"{what}: one dtype, batch, number of tokens and head dimension for all tensors, results and gradients "
                           "of their sources' shapes")
-    return TENSOR.pack(x.data_ptr(), OUT_DTYPES[dtype], b, h, n)
+    return TENSOR.pack(x.data_ptr(), OUT_DTYPES[dtype], stride[0], stride[1], stride[2])
 
 
 def _status_ptr(x, what: str):
@@ -500,7 +500,7 @@ def _status_ptr(x, what: str):
 def _vector(x, dim: int, what: str) -> int:
     if x is None:
         return 0
-    if x.dtype != torch.float32 or x.dim() != 1 or x.numel() != dim or not x.is_contiguous():
+    if x.dtype is not torch.float32 or x.shape != (dim,) or not x.is_contiguous():
         raise Lite3rError(f"{what}: weights, biases and their gradients must be contiguous float32 vectors of their dimension")
     return x.data_ptr()
 
@@ -598,7 +598,7 @@ class MxTensor:
         codes = rows * (width if self.format == "mxfp8" else width // 2)
         scales = -(-rows // 128) * -(-width // 128) * 512
         for x, size in ((self.codes, codes), (self.scales, scales)):
-            if x.dtype != torch.uint8 or not x.is_contiguous() or x.numel() != size:
+            if x.dtype is not torch.uint8 or x.numel() != size or not x.is_contiguous():
                 raise Lite3rError(f"{what}: codes and scales must be contiguous uint8 tensors of a [{rows}, {width}] matrix")
         if cols is not None and cols != width:
             raise Lite3rError(f"{what}: operands disagree about d_in")
@@ -615,7 +615,7 @@ def lite3r_mx_sizes(format: str, rows: int, cols: int):
 
 
 def alloc_mx(rows: int, cols: int, format: str, device) -> MxTensor:
-    """Buffers of a microscaled matrix, both in one piece of memory (a second allocation costs as much as the launch)."""
+    """Buffers of a microscaled matrix, both in one piece of memory (a second allocation costs more than the two views)."""
     if format not in MX_FORMATS or rows <= 0 or cols <= 0 or cols % 32:
         lite3r_mx_sizes(format, rows, cols)  # refuses what has no such form
     row_tiles, col_tiles, pitch = -(-rows // 128), -(-cols // 128), cols if format == "mxfp8" else cols // 2
@@ -625,18 +625,20 @@ def alloc_mx(rows: int, cols: int, format: str, device) -> MxTensor:
                     both.as_strided((row_tiles, col_tiles, 32, 4, 4), (col_tiles * 512, 512, 16, 4, 1)), rows, cols, format)
 
 
-def _matrix(x, what: str, dtypes=OUT_DTYPES) -> int:
-    if x.dim() != 2 or x.stride(1) != 1 or x.dtype not in dtypes:
+def _matrix(x, what: str, dtypes=OUT_DTYPES):
+    """(dtype's code, row stride) of a matrix with contiguous columns."""
+    stride, dtype = x.stride(), x.dtype
+    if len(stride) != 2 or stride[1] != 1 or dtype not in dtypes:
         names = " / ".join(str(t).replace("torch.", "") for t in dtypes)
         raise Lite3rError(f"{what}: matrices must be {names} with contiguous columns")
-    return OUT_DTYPES[x.dtype]
+    return OUT_DTYPES[dtype], stride[0]
 
 
 def lite3r_quantize_mx(x: torch.Tensor, format: str = "mxfp4", out=None, stream=None) -> MxTensor:
     """Microscaled form of a CUDA matrix [rows, cols] (fp32 / bf16 / fp16, contiguous columns, cols a multiple of 32):
     "mxfp4" for operands of lite3r_linear_mxfp4, "mxfp8" for activations kept for the backward pass.  out: an MxTensor to fill."""
     what = "lite3r_quantize_mx"
-    dtype = _matrix(x, what)
+    dtype, pitch = _matrix(x, what)
     rows, cols = x.shape
     if out is None:
         _on_current_device(what, x)
@@ -650,7 +652,7 @@ def lite3r_quantize_mx(x: torch.Tensor, format: str = "mxfp4", out=None, stream=
             raise Lite3rError(f"{what}: out has another shape or format")
         out.check(what)
         _on_current_device(what, x, out.codes, out.scales)
-    _check(lib().lite3r_quantize_mx(x.data_ptr(), dtype, x.stride(0), rows, cols, MX_FORMATS[format], out.codes.data_ptr(),
+    _check(lib().lite3r_quantize_mx(x.data_ptr(), dtype, pitch, rows, cols, MX_FORMATS[format], out.codes.data_ptr(),
                                     out.scales.data_ptr(), _stream_ptr(stream)), what)
     return out
 
@@ -658,12 +660,13 @@ def lite3r_quantize_mx(x: torch.Tensor, format: str = "mxfp4", out=None, stream=
 def lite3r_dequantize_mx(t: MxTensor, out: torch.Tensor, stream=None) -> torch.Tensor:
     """The values that `t` stands for, into `out` (CUDA [rows, cols] fp32 / bf16 / fp16), which is returned."""
     what = "lite3r_dequantize_mx"
-    dtype, code = _matrix(out, what), t.check(what)
-    _on_current_device(what, out, t.codes, t.scales)
-    if tuple(out.shape) != (t.rows, t.cols):
-        raise Lite3rError(f"{what}: out must be [{t.rows}, {t.cols}]")
-    _check(lib().lite3r_dequantize_mx(t.codes.data_ptr(), t.scales.data_ptr(), code, t.rows, t.cols, out.data_ptr(), dtype,
-                                      out.stride(0), _stream_ptr(stream)), what)
+    (dtype, pitch), code = _matrix(out, what), t.check(what)
+    codes, scales, rows, cols = t.codes, t.scales, t.rows, t.cols
+    _on_current_device(what, out, codes, scales)
+    if out.shape != (rows, cols):
+        raise Lite3rError(f"{what}: out must be [{rows}, {cols}]")
+    _check(lib().lite3r_dequantize_mx(codes.data_ptr(), scales.data_ptr(), code, rows, cols, out.data_ptr(), dtype, pitch,
+                                      _stream_ptr(stream)), what)
     return out
 
 
@@ -671,14 +674,16 @@ def lite3r_linear_mxfp4(x: MxTensor, w: MxTensor, bias, y: torch.Tensor, device_
     """y = Q(x) Q(W)^T + b on MXFP4 operands ([rows, d_in] x [d_out, d_in]); y: CUDA [rows, d_out] fp32 / bf16 / fp16;
     bias: fp32 [d_out] or None."""
     what = "lite3r_linear_mxfp4"
-    dtype = _matrix(y, what)
-    x.check(what, format="mxfp4"), w.check(what, cols=x.cols, format="mxfp4")
-    _on_current_device(what, x.codes, x.scales, w.codes, w.scales, bias, y, device_status)
-    if tuple(y.shape) != (x.rows, w.rows):
-        raise Lite3rError(f"{what}: y must be [{x.rows}, {w.rows}]")
-    _check(lib().lite3r_linear_mxfp4(x.codes.data_ptr(), x.scales.data_ptr(), w.codes.data_ptr(), w.scales.data_ptr(),
-                                     _vector(bias, w.rows, what), x.rows, x.cols, w.rows, y.data_ptr(), dtype, y.stride(0),
-                                     _status_ptr(device_status, what), _stream_ptr(stream)), what)
+    dtype, pitch = _matrix(y, what)
+    rows, d_in, d_out = x.rows, x.cols, w.rows
+    x.check(what, format="mxfp4"), w.check(what, cols=d_in, format="mxfp4")
+    xc, xs, wc, ws = x.codes, x.scales, w.codes, w.scales
+    _on_current_device(what, xc, xs, wc, ws, y, bias, device_status)
+    if y.shape != (rows, d_out):
+        raise Lite3rError(f"{what}: y must be [{rows}, {d_out}]")
+    _check(lib().lite3r_linear_mxfp4(xc.data_ptr(), xs.data_ptr(), wc.data_ptr(), ws.data_ptr(), _vector(bias, d_out, what), rows,
+                                     d_in, d_out, y.data_ptr(), dtype, pitch, _status_ptr(device_status, what),
+                                     _stream_ptr(stream)), what)
 
 
 def lite3r_linear_mx_workspace(rows: int, d_in: int, d_out: int) -> int:
@@ -691,14 +696,15 @@ def lite3r_linear_mx_dgrad(dy: torch.Tensor, w: MxTensor, dx: torch.Tensor, devi
     """dx = dy . Q(W): gradient of a linear layer's input through its microscaled weight [d_out, d_in].  dy: CUDA bf16
     [rows, d_out]; dx: CUDA [rows, d_in] fp32 / bf16 / fp16."""
     what = "lite3r_linear_mx_dgrad"
-    _matrix(dy, what, (torch.bfloat16,))
-    dtype, code = _matrix(dx, what), w.check(what)
+    _, dy_pitch = _matrix(dy, what, (torch.bfloat16,))
+    (dtype, dx_pitch), code = _matrix(dx, what), w.check(what)
     _on_current_device(what, dy, w.codes, w.scales, dx, device_status)
-    if dy.shape[1] != w.rows or tuple(dx.shape) != (dy.shape[0], w.cols):
-        raise Lite3rError(f"{what}: dy must be [rows, {w.rows}] and dx [rows, {w.cols}]")
-    _check(lib().lite3r_linear_mx_dgrad(dy.data_ptr(), dy.stride(0), w.codes.data_ptr(), w.scales.data_ptr(), code, dy.shape[0],
-                                        w.cols, w.rows, dx.data_ptr(), dtype, dx.stride(0),
-                                        _status_ptr(device_status, what), _stream_ptr(stream)), what)
+    rows, d_out = dy.shape
+    d_in = w.cols
+    if d_out != w.rows or dx.shape != (rows, d_in):
+        raise Lite3rError(f"{what}: dy must be [rows, {w.rows}] and dx [rows, {d_in}]")
+    _check(lib().lite3r_linear_mx_dgrad(dy.data_ptr(), dy_pitch, w.codes.data_ptr(), w.scales.data_ptr(), code, rows, d_in, d_out,
+                                        dx.data_ptr(), dtype, dx_pitch, _status_ptr(device_status, what), _stream_ptr(stream)), what)
 
 
 def lite3r_linear_mx_wgrad(dy: torch.Tensor, x: MxTensor, dw: torch.Tensor, db, workspace: torch.Tensor, device_status=None,
@@ -706,15 +712,16 @@ def lite3r_linear_mx_wgrad(dy: torch.Tensor, x: MxTensor, dw: torch.Tensor, db, 
     """dw = dy^T . C(x) (CUDA fp32 [d_out, d_in], contiguous) and db = sum of dy over the rows (fp32 [d_out], or None) from
     the kept form C(x) of the layer's input [rows, d_in].  workspace: lite3r_linear_mx_workspace(rows, d_in, d_out) bytes."""
     what = "lite3r_linear_mx_wgrad"
-    _matrix(dy, what, (torch.bfloat16,))
+    _, dy_pitch = _matrix(dy, what, (torch.bfloat16,))
     code = x.check(what)
-    _on_current_device(what, dy, x.codes, x.scales, dw, db, workspace, device_status)
-    if dy.shape[0] != x.rows or dw.dtype != torch.float32 or not dw.is_contiguous() or tuple(dw.shape) != (dy.shape[1], x.cols):
-        raise Lite3rError(f"{what}: dy must be [{x.rows}, d_out] and dw contiguous float32 [d_out, {x.cols}]")
-    _check(lib().lite3r_linear_mx_wgrad(dy.data_ptr(), dy.stride(0), x.codes.data_ptr(), x.scales.data_ptr(), code, x.rows, x.cols,
-                                        dy.shape[1], dw.data_ptr(), _vector(db, dy.shape[1], what), workspace.data_ptr(),
-                                        _bytes_of(workspace, what), _status_ptr(device_status, what),
-                                        _stream_ptr(stream)), what)
+    _on_current_device(what, dy, x.codes, x.scales, dw, workspace, db, device_status)
+    rows, d_out = dy.shape
+    d_in = x.cols
+    if rows != x.rows or dw.dtype != torch.float32 or not dw.is_contiguous() or dw.shape != (d_out, d_in):
+        raise Lite3rError(f"{what}: dy must be [{x.rows}, d_out] and dw contiguous float32 [d_out, {d_in}]")
+    _check(lib().lite3r_linear_mx_wgrad(dy.data_ptr(), dy_pitch, x.codes.data_ptr(), x.scales.data_ptr(), code, rows, d_in, d_out,
+                                        dw.data_ptr(), _vector(db, d_out, what), workspace.data_ptr(), _bytes_of(workspace, what),
+                                        _status_ptr(device_status, what), _stream_ptr(stream)), what)
 
 
 # ----------------------------------------------------------------------------- training side of the projection
