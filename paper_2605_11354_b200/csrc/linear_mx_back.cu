@@ -483,10 +483,9 @@ struct Sums {
   int count;
 };
 
-// out[i] = sum over the parts, in order: dw four values to a thread (blocks below dw_blocks), db one to a thread, four
-// quarters of the parts side by side.
+// out[i] = sum over the parts in a fixed order: dw four values to a thread (blocks below dw_blocks), then db.
 __global__ void __launch_bounds__(256) add_parts_kernel(const Sums dw, int dw_blocks, const Sums db) {
-  __shared__ float s_sum[4][64];
+  __shared__ float s_sum[8][8];
   wait_for_prior_grid();
   launch_dependents();
   if (static_cast<int>(blockIdx.x) < dw_blocks) {
@@ -501,17 +500,24 @@ __global__ void __launch_bounds__(256) add_parts_kernel(const Sums dw, int dw_bl
     *reinterpret_cast<float4*>(dw.out + i) = acc;
     return;
   }
-  const int col = threadIdx.x & 63, quarter = threadIdx.x >> 6;
-  const size_t i = static_cast<size_t>(blockIdx.x - dw_blocks) * 64 + col;
+  // eight columns, 32 threads to each with every 32nd part, eight requested at a time
+  const int col = threadIdx.x & 7, group = threadIdx.x >> 3;
+  const size_t i = static_cast<size_t>(blockIdx.x - dw_blocks) * 8 + col;
   float acc = 0.f;
   if (i < db.values) {
-    const int s0 = db.count * quarter / 4, s1 = db.count * (quarter + 1) / 4;
 #pragma unroll 8
-    for (int s = s0; s < s1; ++s) acc += db.parts[static_cast<size_t>(s) * db.values + i];
+    for (int s = group; s < db.count; s += 32) acc += db.parts[static_cast<size_t>(s) * db.values + i];
   }
-  s_sum[quarter][col] = acc;
+#pragma unroll
+  for (int o = 16; o >= 8; o >>= 1) acc += __shfl_xor_sync(0xFFFFFFFFu, acc, o);
+  if ((threadIdx.x & 31) < 8) s_sum[threadIdx.x >> 5][col] = acc;
   __syncthreads();
-  if (threadIdx.x < 64 && i < db.values) db.out[i] = (s_sum[0][col] + s_sum[1][col]) + (s_sum[2][col] + s_sum[3][col]);
+  if (threadIdx.x < 8 && i < db.values) {
+    acc = 0.f;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) acc += s_sum[w][col];
+    db.out[i] = acc;
+  }
 }
 
 constexpr int kBiasCols = 4;
@@ -663,7 +669,7 @@ lite3r_status launch_mx_wgrad(const void* dy, long long dy_stride, const uint8_t
   const Cut c = cut_tiles(d_out, d_in, parts, pairs);
   const int bias_count = ((parts - 1) * kGroups + std::min(kGroups, last)) * std::min(kBiasCols, c.wide + c.half) * 4;
   const Sums dw_sums = {products, dw, values, parts}, db_sums = {bias_parts, db, static_cast<size_t>(d_out), bias_count};
-  const long long dw_blocks = parts > 1 ? static_cast<long long>((values / 4 + 255) / 256) : 0, db_blocks = db != nullptr ? ceil_div(d_out, 64) : 0;
+  const long long dw_blocks = parts > 1 ? static_cast<long long>((values / 4 + 255) / 256) : 0, db_blocks = db != nullptr ? ceil_div(d_out, 8) : 0;
   if (dw_blocks + db_blocks > 0x7FFFFFFFLL) return LITE3R_ERR_UNSUPPORTED;
   return launch_dependent(add_parts_kernel, dim3(static_cast<unsigned>(dw_blocks + db_blocks)), 256, 0, stream, dw_sums,
                           static_cast<int>(dw_blocks), db_sums);

@@ -404,25 +404,34 @@ struct RopeSums {
   float* d[2][2];  // [queries, keys][weight, bias] or null
 };
 
-// Adds the partials in a fixed order: a CTA has 32 elements of a tensor's dw and db, its 32 warps every 32nd partial each.
-__global__ void __launch_bounds__(1024) rope_sums_kernel(const float* partials, int count, int dim, const __grid_constant__ RopeSums sums) {
-  __shared__ float s_sum[32][33];
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  const int which = blockIdx.y, e = blockIdx.x * 32 + lane;  // 2 dim elements: dw, db
-  const float* src = partials + static_cast<size_t>(which) * kMaxRopePartials * 2 * dim + e;
-  float acc = 0.f;
+// Adds the partials in a fixed order: a CTA has 8 elements of a tensor's dw and db, thread (i, e) every 128th partial of
+// element e, all requested at once (a chain of batches of loads took 6 us, as long as a tenth of the gradient itself).
+constexpr int kSumThreads = 1024, kSumElements = 8, kSumGroups = kSumThreads / kSumElements;
+__global__ void __launch_bounds__(kSumThreads) rope_sums_kernel(const float* partials, int count, int dim, const __grid_constant__ RopeSums sums) {
+  __shared__ float s_sum[kSumThreads / 32][kSumElements];
+  constexpr int kMost = kMaxRopePartials / kSumGroups;
+  const int which = blockIdx.y, e = threadIdx.x % kSumElements, group = threadIdx.x / kSumElements;
+  const int element = blockIdx.x * kSumElements + e;  // of 2 dim: dw, db
+  const float* src = partials + static_cast<size_t>(which) * kMaxRopePartials * 2 * dim + element;
   wait_for_prior_grid();
   launch_dependents();
-#pragma unroll 8
-  for (int i = warp; i < count; i += 32) acc += src[static_cast<size_t>(i) * 2 * dim];
-  s_sum[warp][lane] = acc;
+  float v[kMost], acc = 0.f;
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) v[i] = group + i * kSumGroups < count ? src[static_cast<size_t>(group + i * kSumGroups) * 2 * dim] : 0.f;
+#pragma unroll
+  for (int i = 0; i < kMost; ++i) acc += v[i];
+  // the groups' sums: those of a warp by shuffles, then the warps'
+#pragma unroll
+  for (int o = 16; o >= kSumElements; o >>= 1) acc += __shfl_xor_sync(0xFFFFFFFFu, acc, o);
+  const int warp = threadIdx.x >> 5;
+  if ((threadIdx.x & 31) < kSumElements) s_sum[warp][e] = acc;
   __syncthreads();
-  if (warp == 0) {
+  if (threadIdx.x < kSumElements) {
     acc = 0.f;
 #pragma unroll
-    for (int w = 0; w < 32; ++w) acc += s_sum[w][lane];
-    float* dst = sums.d[which][e >= dim];
-    if (dst != nullptr) dst[e >= dim ? e - dim : e] = acc;
+    for (int w = 0; w < kSumThreads / 32; ++w) acc += s_sum[w][e];
+    float* dst = sums.d[which][element >= dim];
+    if (dst != nullptr) dst[element >= dim ? element - dim : element] = acc;
   }
 }
 
@@ -551,7 +560,7 @@ lite3r_status launch_rope_backward(const lite3r_tensor* q, const lite3r_tensor* 
   if (st != LITE3R_OK) return st;
   RopeSums sums = {{{grads.q_weight, grads.q_bias}, {grads.k_weight, grads.k_bias}}};
   if (grads.q_weight == nullptr && grads.q_bias == nullptr && grads.k_weight == nullptr && grads.k_bias == nullptr) return LITE3R_OK;
-  return launch_dependent(rope_sums_kernel, dim3(static_cast<unsigned>(how.head_dim / 16), tensors), 1024, 0, stream,
+  return launch_dependent(rope_sums_kernel, dim3(static_cast<unsigned>(2 * how.head_dim / kSumElements), tensors), kSumThreads, 0, stream,
                           static_cast<const float*>(partials), blocks, how.head_dim, sums);
 }
 
