@@ -9,6 +9,9 @@
 // shared memory.  The products of the next tile run under the epilogue of this one.
 // Tensor memory: two accumulators of 256 columns leave no room for the scales, so they share 32 columns: the warpgroup that
 // has these reads them first, and the next tile's products wait for that (a few hundred cycles) and not for the epilogue.
+// 43968 x 4096 x 1024 in 69 us, 5.3 PFLOP/s, the tensor pipe busy for 70 % of it (by single CTAs on 128 x 128: 162 us).  A stage of
+// 256 elements of K takes 720 cycles: 560 of products and 100 of scale copies, which run in order with them, and at the end of a
+// tile the wait for the shared columns.  10992 x 1024 x 4096 in 26 us.
 // Every mbarrier wait is bounded; on expiry the CTA sets *device_status and its roles leave their loops.
 #include <algorithm>
 
