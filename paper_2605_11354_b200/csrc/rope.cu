@@ -487,7 +487,8 @@ RopeParams params_of(const lite3r_rope& how) {
 void set_chunks(RopeTensor& t, long long tokens_all, int dim, int most, int sms, int ctas) {
   if (t.heads == 0) return;
   const long long groups = static_cast<long long>(sms) * ctas * (kRopeThreads / (dim / 16));
-  const int chunk = static_cast<int>(std::min<long long>(std::min(most, t.heads), std::max<long long>(1, tokens_all * t.heads / groups)));
+  int chunk = static_cast<int>(std::min<long long>(std::min(most, t.heads), std::max<long long>(1, tokens_all * t.heads / groups)));
+  chunk = std::max(chunk, ceil_div(t.heads, 32767));  // (parts are the grid's second dimension)
   t.chunks = ceil_div(t.heads, chunk);
   t.chunk = ceil_div(t.heads, t.chunks);
 }
