@@ -352,7 +352,8 @@ __global__ void __launch_bounds__(kRopeThreads, back_ctas(sizeof(T))) rope_back_
       next_x.values(xa, xb);
       next_g.values(ga, gb);
       if (i + 1 < t.chunk) fetch(i + 1);
-      const float r1 = centre<kDim>(xa, xb, p.norm, p.eps);
+      const float root = centre<kDim>(xa, xb, p.norm, p.eps);
+      const float r1 = i < count ? root : 0.f;  // (rows past the end are zeros; without an epsilon their root is infinite)
       const F2 r = both(r1);
       const ulonglong2* const w = reinterpret_cast<const ulonglong2*>(s_weight);
       F2 m1 = 0ull, m2 = 0ull;

@@ -1,0 +1,162 @@
+"""The parts of the operators around the attention that only large calls run -- several heads to a group of lanes, several
+steps of the grid, pairs of CTAs over many tiles -- and the settings at the ends of what the calls accept.
+
+The rows of test_gpu_layer_ops are few enough that every head of a token has a group of lanes of its own; here they are not.
+References are in fp64, by complex numbers on the device; sums over rows are of whole numbers, which fp32 adds exactly, so that one
+row too many or too few is seen.
+"""
+import numpy as np
+import pytest
+import torch
+
+import test_gpu_layer_ops as base
+from paper_2605_11354_b200 import binding as lt
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+DTYPES = base.DTYPES
+
+
+def turned(z, positions, base_, back=False):
+    """The rotation of z [B, H, N, D] (fp64) by positions [B, N, axes]: a pair is a complex number."""
+    axes = positions.shape[-1]
+    half = z.shape[-1] // axes // 2
+    angle = positions.double()[:, None, :, :, None] * base_ ** (-torch.arange(half, device=z.device, dtype=torch.float64) / half)
+    a, b = z.view(*z.shape[:3], axes, 2, half).unbind(-2)
+    c = torch.complex(a, b) * torch.polar(torch.ones_like(angle), -angle if back else angle)
+    return torch.stack([c.real, c.imag], -2).reshape(z.shape)
+
+
+def normed(x, norm, eps):
+    if norm == "none":
+        return x, torch.ones_like(x[..., :1])
+    if norm == "layer":
+        x = x - x.mean(-1, keepdim=True)
+    r = 1 / torch.sqrt(x.square().mean(-1, keepdim=True) + eps)
+    return x * r, r
+
+
+def all_within(got, ref, tol, dtype, what):
+    """As within() of the other file, on the device; nothing here comes near the end of a type."""
+    half = torch.finfo(dtype).eps / 2
+    tol = tol + half * (ref.abs() + tol) + base.TINY[dtype]
+    worst = ((got.double() - ref).abs() / tol).max().item()
+    assert worst <= 1.0, (what, worst)
+
+
+# ------------------------------------------------------------------------------------------------------ walks over heads
+# B, H, K, N, D, axes, norm, dtype.  With 148 SMs the forward gives a group of lanes
+#   3 of 10 heads and 1 of 5;   12 of 24 and 4 of 7;   16 of 16;   4 of 7 and 2 of 3;   3 of 5 and 12 of 24
+# and of the last two 3 and 1, 5;  the gradient 4 and 2;  4 and 4;  4;  4 and 3;  3 and 4;  4 and 3;  3, in two to nine steps of the grid.
+WALKS = [(3, 10, 5, 3001, 64, 1, "rms", "bf16"), (2, 24, 7, 10000, 64, 2, "layer", "bf16"), (1, 16, 16, 32003, 64, 2, "layer", "f16"),
+         (1, 7, 3, 10007, 128, 1, "rms", "f16"), (4, 5, 24, 10001, 32, 2, "layer", "f32"), (3, 10, 5, 3001, 64, 0, "layer", "f32"),
+         (1, 5, 5, 9001, 256, 2, "none", "f32")]
+
+
+@pytest.mark.parametrize("B,H,K,N,D,axes,norm,dtype", WALKS)
+def test_rows_of_a_walk(B, H, K, N, D, axes, norm, dtype):
+    eps, turn_base = 1e-5, 100.0
+    q, k = base.rope_inputs(41, B, H, K, N, D, DTYPES[dtype], "packed")
+    dqo, dko = base.rope_inputs(42, B, H, K, N, D, DTYPES[dtype], "heads")
+    qw, qb, kw, kb = base.affine(43, D)
+    pos = torch.randint(-40, 1400, (B, N, axes), generator=torch.Generator().manual_seed(44)).int().cuda() if axes else None
+    how = dict(norm=norm, positions=pos, base=turn_base, eps=eps)
+    out = [torch.full(x.shape, 9.0, dtype=x.dtype, device="cuda") for x in (q, k)]
+    lt.lite3r_qk_norm_rope(q, k, *out, q_weight=qw, q_bias=qb, k_weight=kw, k_bias=kb, **how)
+    grads = [torch.full(x.shape, 9.0, dtype=x.dtype, device="cuda") for x in (q, k)]
+    lt.lite3r_qk_norm_rope_backward(q, k, dqo, dko, *grads, base.workspace(lt.lite3r_qk_norm_rope_workspace(D)), q_weight=qw, k_weight=kw, **how)
+    roundings = 32 if dtype == "f32" else 46  # the counts of test_gpu_layer_ops
+    for x, y, dy, dx, w, b, name in ((q, out[0], dqo, grads[0], qw, qb, "q"), (k, out[1], dko, grads[1], kw, kb, "k")):
+        for h in range(x.shape[1]):
+            x64, dy64 = x[:, h:h + 1].double(), dy[:, h:h + 1].double()
+            xh, r = normed(x64, norm, eps)
+            z = xh * w + b
+            ref = z if pos is None else turned(z, pos, turn_base)
+            top = x64.abs().amax(-1, keepdim=True) * r
+            all_within(y[:, h:h + 1], ref, roundings * U * (top * w.abs().max() + b.abs().max()), y.dtype, (name, h))
+            g = dy64 if pos is None else turned(dy64, pos, turn_base, back=True)
+            gh = g * w
+            d = gh
+            if norm != "none":
+                d = gh - xh * (gh * xh).mean(-1, keepdim=True)
+                d = (d - gh.mean(-1, keepdim=True) if norm == "layer" else d) * r
+            a = 2 * dy64.abs().amax(-1, keepdim=True) * w.abs().max()
+            all_within(dx[:, h:h + 1], d, 64 * U * r * a * (1 + top + top * top), dx.dtype, (name, h, "dx"))
+
+
+def whole_rows(seed, shape, dtype):
+    """Rows of as many 1 as -1: no mean, variance 1, whole numbers after either norm without an epsilon."""
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    order = torch.rand(shape, generator=g, device="cuda").argsort(-1)
+    return (1 - 2 * (order % 2)).to(dtype)
+
+
+@pytest.mark.parametrize("norm", ["none", "rms", "layer"])
+@pytest.mark.parametrize("B,H,K,N,D,dtype", [(1, 1, 1, 3, 64, "f32"), (2, 3, 2, 37, 32, "bf16"), (1, 8, 2, 1, 256, "f16"), (1, 5, 1, 130, 128, "bf16"),
+                                             (3, 10, 5, 3001, 64, "bf16"), (3, 10, 5, 3001, 64, "f32"), (2, 24, 7, 10000, 64, "f16"),
+                                             (4, 5, 24, 10001, 32, "bf16"), (1, 7, 3, 20011, 128, "f16")])
+def test_sums_without_an_epsilon_count_every_row_once(B, H, K, N, D, dtype, norm):
+    """Gradients of whole numbers in some rows -- the first and last of every head and sequence among them -- and zeros in
+    the rest: adding a zero is exact, and some 300 terms of at most 4 in fp32 in any order, with a root that is off by 2 ulp, are
+    off by at most (300 + 4) u of a sum of magnitudes below 1200: 0.03.  A row lost, doubled or taken from its
+    neighbour is off by 1 or more in half of the elements.  Rows of zeros have no deviation: at eps = 0 they may not be looked at."""
+    args = []
+    for heads, seed in ((H, 1), (K, 2)):
+        x = whole_rows(seed, (B, heads, N, D), DTYPES[dtype])
+        g = torch.Generator().manual_seed(seed)
+        dy = torch.zeros(B * heads * N, D)
+        ends = [(b * heads + h) * N + n for b in {0, B - 1} for h in range(heads) for n in (0, N - 1)]
+        rows = torch.unique(torch.cat([torch.tensor(ends), torch.randint(0, B * heads * N, (150,), generator=g)]))
+        assert len(rows) <= 300
+        dy[rows] = torch.randint(1, 5, (len(rows), D), generator=g).float()
+        args.append((x, dy.view(B, heads, N, D).to(DTYPES[dtype]).cuda()))
+    total = [((x.double() * dy.double()).sum((0, 1, 2)), dy.double().sum((0, 1, 2))) for x, dy in args]
+    grads = {n: torch.full((D,), 7.0, device="cuda") for n in ("dq_weight", "dq_bias", "dk_weight", "dk_bias")}
+    for positions in (None, torch.zeros((N, 2), dtype=torch.int32, device="cuda")):  # a turn by nothing is exact, too
+        dx = [torch.empty_like(x) for x, _ in args]
+        lt.lite3r_qk_norm_rope_backward(args[0][0], args[1][0], args[0][1], args[1][1], *dx, base.workspace(lt.lite3r_qk_norm_rope_workspace(D)),
+                                        norm=norm, eps=0.0, positions=positions, **grads)
+        for (dw, db), name in zip(total, "qk"):
+            assert torch.equal(grads[f"d{name}_bias"].double(), db), name
+            off = (grads[f"d{name}_weight"].double() - dw).abs().max().item()
+            assert off <= (0.0 if norm == "none" else 0.03), (name, off)  # (a NaN compares false)
+        assert all(t.isfinite().all() for t in dx)
+
+
+def test_dense_sums_of_whole_numbers():
+    """Every row has a gradient: sums of whole numbers below 2^24 are exact in fp32 in any order."""
+    for B, H, K, N, D, dtype in ((3, 10, 5, 3001, 64, torch.bfloat16), (1, 16, 4, 40003, 64, torch.float16), (2, 6, 6, 9001, 128, torch.float32)):
+        g = torch.Generator(device="cuda").manual_seed(3)
+        ints = lambda heads: torch.randint(-3, 4, (B, heads, N, D), generator=g, device="cuda").to(dtype)  # noqa: E731
+        q, k, dqo, dko = ints(H), ints(K), ints(H), ints(K)
+        grads = {n: torch.full((D,), 7.0, device="cuda") for n in ("dq_weight", "dq_bias", "dk_weight", "dk_bias")}
+        lt.lite3r_qk_norm_rope_backward(q, k, dqo, dko, torch.empty_like(q), torch.empty_like(k),
+                                        base.workspace(lt.lite3r_qk_norm_rope_workspace(D)), norm="none", **grads)
+        for x, dy, name in ((q, dqo, "q"), (k, dko, "k")):
+            assert torch.equal(grads[f"d{name}_weight"].double(), (x.double() * dy.double()).sum((0, 1, 2)))
+            assert torch.equal(grads[f"d{name}_bias"].double(), dy.double().sum((0, 1, 2)))
+
+
+def test_more_heads_than_a_grid_has_parts():
+    """Heads of a token are parts of the grid's second dimension, of which there are 65535: 70000 and 40000 go by threes and twos."""
+    H, K, D = 70000, 40000, 32
+    q, k = base.rope_inputs(5, 1, H, K, 1, D, torch.bfloat16, "heads")
+    pos = torch.tensor([[7]], dtype=torch.int32, device="cuda")
+    out, few = [torch.full_like(x, 9.0) for x in (q, k)], [torch.empty_like(x) for x in (q, k)]
+    lt.lite3r_qk_norm_rope(q, k, *out, positions=pos)
+    for h in range(0, H, 20000):  # as calls of fewer heads
+        lt.lite3r_qk_norm_rope(q[:, h:h + 20000], None, few[0][:, h:h + 20000], None, positions=pos)
+    for h in range(0, K, 20000):
+        lt.lite3r_qk_norm_rope(k[:, h:h + 20000], None, few[1][:, h:h + 20000], None, positions=pos)
+    assert torch.equal(out[0], few[0]) and torch.equal(out[1], few[1])
+    dq, dk = torch.full_like(q, 9.0), torch.full_like(k, 9.0)
+    dw = {n: torch.empty(D, device="cuda") for n in ("dq_weight", "dk_weight")}
+    lt.lite3r_qk_norm_rope_backward(q, k, q, k, dq, dk, base.workspace(lt.lite3r_qk_norm_rope_workspace(D)), norm="none", positions=pos, **dw)
+    for x, d, name in ((q, dq, "q"), (k, dk, "k")):
+        x64, p = x.double(), pos.view(1, 1, 1)
+        g = turned(x64, p, 100.0, back=True)
+        all_within(d, g, 46 * U * 2 * x64.abs().amax(-1, keepdim=True), d.dtype, name)
+        n = x.shape[1]
+        size = (g.abs() * x64.abs()).sum((0, 1, 2))
+        all_within(dw[f"d{name}_weight"], (g * x64).sum((0, 1, 2)), (n + 64) * U * size, torch.float32, name)
