@@ -279,7 +279,9 @@ typedef enum { LITE3R_NORM_NONE = 0, LITE3R_NORM_RMS = 1, LITE3R_NORM_LAYER = 2 
  *   rotation: z is cut into `axes` sections of S = head_dim / axes values, section a turns with coordinate a of the token's
  *   position: the pair (z[i], z[i + S/2]), i < S/2, by the angle position * base^(-2 i / S):
  *     y[i] = z[i] cos - z[i + S/2] sin,   y[i + S/2] = z[i + S/2] cos + z[i] sin.
- * In fp32 (angles in fp64, so that positions of any size keep their angle), rounded once. */
+ * In fp32, rounded once.  Angles are fractions of a turn in 64-bit fixed point, from factors made in fp64, so that positions of any
+ * size keep their angle; 16-bit results of the forward take sines and cosines that are off by at most 2^-20.5, all others
+ * such that are good to fp32. */
 typedef struct {
   int batch, q_heads, k_heads, tokens, head_dim; /* head_dim 32, 64, 128 or 256; k_heads need not equal q_heads; 0: no keys */
   lite3r_norm norm;

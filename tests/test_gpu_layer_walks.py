@@ -160,3 +160,22 @@ def test_more_heads_than_a_grid_has_parts():
         n = x.shape[1]
         size = (g.abs() * x64.abs()).sum((0, 1, 2))
         all_within(dw[f"d{name}_weight"], (g * x64).sum((0, 1, 2)), (n + 64) * U * size, torch.float32, name)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_sums_have_sines_of_fp32(dtype):
+    """The weight and bias gradients are fp32 results of 16-bit sources, too.  A gradient of (1, 0) in every pair of a single row
+    makes the bias gradient (cos, -sin).  The angle is rounded to 24 bits below half a turn: off by at most 2^-26 turns, 1.58 u;
+    sine and cosine are good to one ulp, at most u below 1; nothing is rounded after that."""
+    D, turn_base = 256, 100.0
+    x = torch.ones((1, 1, 1, D), dtype=DTYPES[dtype], device="cuda")
+    dy = torch.zeros_like(x)
+    dy[..., :D // 2] = 1
+    dx, db, ws = torch.empty_like(x), torch.empty(D, device="cuda"), base.workspace(lt.lite3r_qk_norm_rope_workspace(D))
+    worst = 0.0
+    for p in np.random.default_rng(6).integers(-1400, 1400, 60):
+        lt.lite3r_qk_norm_rope_backward(x, None, dy, None, dx, None, ws, norm="none", dq_bias=db, base=turn_base,
+                                        positions=torch.tensor([[p]], dtype=torch.int32, device="cuda"))
+        angle = p * turn_base ** (-np.arange(D // 2) / (D // 2))
+        worst = max(worst, np.abs(base.f64(db) - np.concatenate([np.cos(angle), -np.sin(angle)])).max())
+    assert worst <= 2.7 * U, worst / U
