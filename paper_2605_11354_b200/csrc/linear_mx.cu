@@ -190,8 +190,12 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         const uint32_t acc = tmem + (ab ? L::kAcc1 : 0u);
         // with tiles of 64 columns the weight's scale tile serves two of them: columns 0 and 1, or 2 and 3
         const uint32_t sfb_shift = kN == 64 ? 2u * ((tile % p.col_tiles) & 1) : 0u;
-        if (it >= 2) ok = mbar_wait_clearing(&bars->acc_empty[ab], ((it - 2) >> 1) & 1, abort_flag, p.status, 804);
-        if (L::kShared != 0 && ok && it >= 1) ok = mbar_wait_clearing(&bars->shared_read, (it - 1) & 1, abort_flag, p.status, 805);
+        auto wait_read = [&](uint64_t* bar, uint32_t phase, int code) {  // for the epilogues (of both CTAs)
+          if constexpr (kPair) return mbar_wait_cluster_clearing<true>(bar, phase, abort_flag, p.status, code);
+          else return mbar_wait_clearing(bar, phase, abort_flag, p.status, code);
+        };
+        if (it >= 2) ok = wait_read(&bars->acc_empty[ab], ((it - 2) >> 1) & 1, 804);
+        if (L::kShared != 0 && ok && it >= 1) ok = wait_read(&bars->shared_read, (it - 1) & 1, 805);
         ok = __all_sync(0xFFFFFFFFu, ok);
         tc_fence_after();
         for (int k = 0; ok && k < stages_k; ++k) {
@@ -263,7 +267,7 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
         tc_fence_before();
         __syncwarp();
         if (lane == 0) {
-          if constexpr (kPair) mbar_arrive_cluster_own(cluster_u32(bar, 0));
+          if constexpr (kPair) mbar_arrive_cluster_read(cluster_u32(bar, 0));
           else mbar_arrive(bar);
         }
       };

@@ -53,7 +53,8 @@ struct Layout {
   static constexpr uint32_t kRawBytes = kOffScales + kScaleTile;
   static constexpr uint32_t kOffOut = (kOffRaw + kRaw * kRawBytes + 1023) / 1024 * 1024;  // 4 KB per epilogue warp
   static constexpr uint32_t kOffBar = kOffOut + 4 * 4096;
-  static constexpr uint32_t kSmemBytes = kOffBar + 512;
+  static constexpr uint32_t kOffWords = kOffBar + 256;          // of the first CTA: 16 bytes of each converting warp of the second
+  static constexpr uint32_t kSmemBytes = kOffWords + 256;
   static_assert(kSmemBytes <= 232448, "fits");
 };
 
@@ -64,6 +65,7 @@ struct Bars {
   uint32_t tmem_base;
   int abort;
 };
+static_assert(sizeof(Bars) <= 256, "below the words");
 
 struct BackParams {
   const uint8_t* scales;
@@ -158,7 +160,7 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
     for (int s = 0; s < kOps; ++s) {
       mbar_init(&bars->a_full[s], 1);
       mbar_init(&bars->op_empty[s], 1);
-      mbar_init(&bars->b_full[s], 2 * kGroupThreads / 32);
+      mbar_init(&bars->b_full[s], kGroupThreads / 32);
     }
     for (int b = 0; b < 2; ++b) {
       mbar_init(&bars->acc_full[b], 1);
@@ -280,7 +282,7 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
         const uint32_t idesc = u.half ? idesc_half : idesc_wide;
         for (int k0 = u.first; ok && k0 < u.last; k0 += p.steps_per_sum, ++it) {
           const int ab = it & 1, k1 = min(k0 + p.steps_per_sum, u.last);
-          if (it >= 2) ok = mbar_wait_clearing(&bars->acc_empty[ab], ((it - 2) >> 1) & 1, abort_flag, p.status, 814);
+          if (it >= 2) ok = mbar_wait_cluster_clearing<true>(&bars->acc_empty[ab], ((it - 2) >> 1) & 1, abort_flag, p.status, 814);
           ok = __all_sync(0xFFFFFFFFu, ok);
           tc_fence_after();
           for (int k = k0; ok && k < k1; ++k) {
@@ -310,6 +312,7 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
     const int group = (warp - 4) >> 2, t = threadIdx.x & (kGroupThreads - 1);
     const int row = t >> 2, chunk = t & 3;  // of 32 rows and four chunks of sixteen columns at a time
     const uint32_t my_raw = smem_u32(smem) + L::kOffRaw + row * L::kBoxBytes + chunk * Codes<kFormat>::kBytes;
+    const uint32_t word = cluster_u32(smem + L::kOffWords + (warp - 4) * 16, 0);
     const uint32_t my_scales = smem_u32(smem) + L::kOffRaw + L::kOffScales + row * 16;
     const uint32_t my_b = smem_u32(smem) + L::kOffB + row * 128 + (((2 * chunk) ^ (row & 7)) << 4);  // and the next chunk's 16 bytes: ^ 16
     bool ok = true;
@@ -379,7 +382,10 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
           }
         }
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster_own(cluster_u32(&bars->b_full[st], 0));
+        if (lane == 0) {  // each warp of the first CTA expects the word of one of the second: 16 bytes of what it has converted
+          if (rank == 0) mbar_arrive_expect_tx(&bars->b_full[st], 16);
+          else bulk_copy_cluster(word, dst, 16, cluster_u32(&bars->b_full[st], 0));
+        }
       }
       kc += steps;
       if (sums && ok && mine < steps) {
@@ -461,7 +467,7 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive_cluster_own(cluster_u32(&bars->acc_empty[ab], 0));
+        if (lane == 0) mbar_arrive_cluster_read(cluster_u32(&bars->acc_empty[ab], 0));
       }
     }
     bulk_wait_group_read0();  // what is staged stays in place until it has been read

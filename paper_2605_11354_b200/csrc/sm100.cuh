@@ -385,11 +385,21 @@ __device__ __forceinline__ uint32_t cluster_u32(const void* p, uint32_t rank) {
 __device__ __forceinline__ void mbar_arrive_cluster(uint32_t cluster_bar) {
   asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
-// The same after writes to this CTA's own shared memory that a product of the pair will read from there, or reads of its own
-// tensor memory that one will write: their order need only hold where they are, in this CTA (a release at cluster scope waits
-// until everything is performed for the whole GPU: 1800 cycles in the converting warps of the backward GEMM).
-__device__ __forceinline__ void mbar_arrive_cluster_own(uint32_t cluster_bar) {
-  asm volatile("mbarrier.arrive.release.cta.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+// After reads of tensor memory that a product of the pair will overwrite, between tc_fence_before() here and tc_fence_after() behind
+// the wait: those two order the reads and the products, the barrier has to say only that the one came before the other.
+__device__ __forceinline__ void mbar_arrive_cluster_read(uint32_t cluster_bar) {
+  asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// From this CTA's shared memory to that of a CTA of the cluster, counted in bytes on a barrier there.  Addresses and size are
+// multiples of 16.  Also a way to hand over what threads of this CTA have written for a product of the pair: after their proxy
+// fences the copy comes behind their writes, and its count on the barrier releases at cluster scope what came before it.  The
+// thread does not wait, where an arrival that releases at cluster scope holds it until everything that it has under way is
+// performed for the whole GPU (1800 cycles in the converting warps of the backward products, 3000 in a warp that does nothing
+// else); an arrival that releases in this CTA alone orders nothing for a thread of the other one.
+__device__ __forceinline__ void bulk_copy_cluster(uint32_t cluster_dst, uint32_t smem_src, uint32_t bytes, uint32_t cluster_bar) {
+  asm volatile("cp.async.bulk.shared::cluster.shared::cta.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+               ::"r"(cluster_dst), "r"(smem_src), "r"(bytes), "r"(cluster_bar)
+               : "memory");
 }
 // 2-D tile load into this CTA's shared memory, counted in bytes on a barrier of either CTA of the pair.
 __device__ __forceinline__ void tma_load_2d_pair(void* smem_dst, const CUtensorMap* map, uint32_t cluster_bar, int x, int y) {
@@ -435,19 +445,30 @@ __device__ __forceinline__ void mma_f16_pair(uint32_t d_tmem, uint64_t a_desc, u
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
-// As mbar_wait_clearing, for a barrier on which threads of the other CTA arrive after writing to their shared memory.
+// As mbar_wait_clearing, for a barrier on which the other CTA's threads or copies arrive.  kRelaxed: with mbar_arrive_cluster_read.
+template <bool kRelaxed = false>
 __device__ __forceinline__ bool mbar_wait_cluster_clearing(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status, int code) {
   uint64_t since = 0;
   uint32_t polls = 0;
   while (true) {
     uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok)
-        : "r"(smem_u32(bar)), "r"(parity)
-        : "memory");
+    if constexpr (kRelaxed) {
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t"
+          "mbarrier.try_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+          "selp.u32 %0, 1, 0, p;\n\t}"
+          : "=r"(ok)
+          : "r"(smem_u32(bar)), "r"(parity)
+          : "memory");
+    } else {
+      asm volatile(
+          "{\n\t.reg .pred p;\n\t"
+          "mbarrier.try_wait.parity.acquire.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+          "selp.u32 %0, 1, 0, p;\n\t}"
+          : "=r"(ok)
+          : "r"(smem_u32(bar)), "r"(parity)
+          : "memory");
+    }
     if (ok != 0) return true;
     if ((++polls & 0x3Fu) == 0 && (since = wait_check(since, abort_flag, nullptr, code, kWaitLimitNs)) == 0) {
       if (status != nullptr) atomicCAS(status, 0, code);

@@ -179,3 +179,59 @@ def test_sums_have_sines_of_fp32(dtype):
         angle = p * turn_base ** (-np.arange(D // 2) / (D // 2))
         worst = max(worst, np.abs(base.f64(db) - np.concatenate([np.cos(angle), -np.sin(angle)])).max())
     assert worst <= 2.7 * U, worst / U
+
+
+# ------------------------------------------------------------------------------------------------------ pairs of CTAs
+@pytest.mark.parametrize("rows,d_in,d_out,dtype", [(20000, 256, 1024, "bf16"), (10007, 288, 1003, "f32"), (5001, 2080, 2056, "f16"),
+                                                   (43968, 64, 256, "bf16"), (2048, 4096, 5120, "f32")])
+def test_pairs_give_the_same_bits_each_time(rows, d_in, d_out, dtype):
+    """Many tiles of 256 x 256 to a pair, from one stage of operands to a tile to many: what one CTA hands to the other, and the
+    columns that two accumulators share.  A part of the rows and columns against the definition."""
+    x, xv = base.mx_matrix(1, rows, d_in, "mxfp4")
+    w, wv = base.mx_matrix(2, d_out, d_in, "mxfp4")
+    pitch = -(-d_out // 8) * 8
+    first, y = (torch.full((rows, pitch), 5.0, dtype=DTYPES[dtype], device="cuda")[:, :d_out] for _ in range(2))
+    lt.lite3r_linear_mxfp4(x, w, None, first)
+    r, c = (np.unique(np.concatenate([np.arange(0, n, max(1, n // 150)), [n - 1]])) for n in (rows, d_out))
+    ref, size = xv[r] @ wv[c].T, np.abs(xv[r]) @ np.abs(wv[c]).T
+    base.within(first[torch.from_numpy(r).cuda()][:, torch.from_numpy(c).cuda()], ref, 2 * U * (d_in / 64 + 2) * size, DTYPES[dtype], "y")
+    differing = torch.zeros((), dtype=torch.int64, device="cuda")
+    for _ in range(100):
+        lt.lite3r_linear_mxfp4(x, w, None, y)
+        differing += (y != first).sum()
+    assert int(differing.item()) == 0
+
+
+@pytest.mark.parametrize("rows,d_in,d_out,w_fmt,x_fmt", [(3000, 1024, 4096, "mxfp4", "mxfp8"), (5003, 2080, 1000, "mxfp8", "mxfp4"),
+                                                         (20000, 512, 264, "mxfp4", "mxfp8")])
+def test_backward_pairs_give_the_same_bits_each_time(rows, d_in, d_out, w_fmt, x_fmt):
+    """Contractions long enough to go round the rings of stages many times, from two streams at once."""
+    w, wv = base.mx_matrix(1, d_out, d_in, w_fmt)
+    x, xv = base.mx_matrix(2, rows, d_in, x_fmt)
+    dy = torch.randn((rows, d_out), generator=torch.Generator().manual_seed(rows)).bfloat16().cuda()
+    ws = [base.workspace(lt.lite3r_linear_mx_workspace(rows, d_in, d_out)) for _ in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+
+    def results():
+        return [torch.full(s, 5.0, dtype=t, device="cuda") for s, t in (((rows, d_in), torch.bfloat16), ((d_out, d_in), torch.float32),
+                                                                        ((d_out,), torch.float32))]
+
+    first, again = results(), [results() for _ in range(2)]
+    lt.lite3r_linear_mx_dgrad(dy, w, first[0])
+    lt.lite3r_linear_mx_wgrad(dy, x, first[1], first[2], ws[0])
+    r, c = np.arange(0, rows, max(1, rows // 150)), np.arange(0, d_out, max(1, d_out // 150))
+    g = base.f64(dy)
+    base.within(first[0][torch.from_numpy(r).cuda()], g[r] @ wv, 2 * U * (d_out / 16 + 8) * (np.abs(g[r]) @ np.abs(wv)), torch.bfloat16, "dx")
+    base.within(first[1][torch.from_numpy(c).cuda()], g[:, c].T @ xv, 2 * U * (min(rows, 2048) / 16 + rows / 1024 + 8) * (np.abs(g[:, c]).T @ np.abs(xv)),
+                torch.float32, "dw")
+    torch.cuda.synchronize()
+    differing = [torch.zeros(3, dtype=torch.int64, device="cuda") for _ in range(2)]
+    torch.cuda.synchronize()
+    for _ in range(50):
+        for i, stream in enumerate(streams):
+            with torch.cuda.stream(stream):
+                lt.lite3r_linear_mx_dgrad(dy, w, again[i][0])
+                lt.lite3r_linear_mx_wgrad(dy, x, again[i][1], again[i][2], ws[i])
+                differing[i] += torch.stack([(a != b).sum() for a, b in zip(again[i], first)])
+    torch.cuda.synchronize()
+    assert not any(d.any() for d in differing), differing
