@@ -46,6 +46,10 @@ LITE3R_API lite3r_status lite3r_plan_variant(int variant);
  * stores, so that both ways can be compared; on == 0 restores the default.  Process-wide. */
 LITE3R_API lite3r_status lite3r_attention_plain_stores(int on);
 
+/* The parts into which lite3r_linear_mx_wgrad cuts the rows on a device with this many SMs, and the bytes of its workspace that it
+ * then uses.  Host-only. */
+LITE3R_API lite3r_status lite3r_linear_mx_parts(int rows, int d_in, int d_out, int sms, int* parts, size_t* bytes);
+
 /* Byte offsets, inside the workspace of lite3r_sla_forward, of its six parts, for tests that inspect intermediates
  * after a forward: offsets[0] per-key-block summaries, bf16 [tiles][4160] = ((H_j W)^T as [e][d] | z_j[d]), the
  * KV summary and normaliser of Algorithm 1 per block with the projection folded in; [1] per-query-block aggregates

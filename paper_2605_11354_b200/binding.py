@@ -71,7 +71,7 @@ EXPORTS = ("lite3r_fp8_sizes", "lite3r_plan_sizes", "lite3r_forward_workspace", 
            "lite3r_plan_variant", "lite3r_attention_plain_stores", "lite3r_sla_step",
            "lite3r_qk_norm_rope", "lite3r_qk_norm_rope_workspace", "lite3r_qk_norm_rope_backward", "lite3r_mx_sizes",
            "lite3r_quantize_mx", "lite3r_dequantize_mx", "lite3r_linear_mxfp4", "lite3r_linear_mx_workspace",
-           "lite3r_linear_mx_dgrad", "lite3r_linear_mx_wgrad")
+           "lite3r_linear_mx_dgrad", "lite3r_linear_mx_wgrad", "lite3r_linear_mx_parts")
 STATIC_SCRATCH_BYTES = 32 << 20  # LITE3R_STATIC_SCRATCH_BYTES
 
 
@@ -148,6 +148,7 @@ def lib() -> C.CDLL:
             "lite3r_dequantize_mx": [vp, vp, C.c_int, C.c_int, C.c_int, vp, C.c_int, ll, vp],
             "lite3r_linear_mxfp4": [vp, vp, vp, vp, vp, C.c_int, C.c_int, C.c_int, vp, C.c_int, ll, vp, vp],
             "lite3r_linear_mx_workspace": [C.c_int, C.c_int, C.c_int, sz],
+            "lite3r_linear_mx_parts": [C.c_int, C.c_int, C.c_int, C.c_int, C.POINTER(C.c_int), sz],
             "lite3r_linear_mx_dgrad": [vp, ll, vp, vp, C.c_int, C.c_int, C.c_int, C.c_int, vp, C.c_int, ll, vp, vp],
             "lite3r_linear_mx_wgrad": [vp, ll, vp, vp, C.c_int, C.c_int, C.c_int, C.c_int, vp, vp, vp, C.c_size_t, vp, vp]}.items():
         getattr(L, name).argtypes = argtypes
@@ -690,6 +691,13 @@ def lite3r_linear_mx_workspace(rows: int, d_in: int, d_out: int) -> int:
     a = C.c_size_t()
     _check(lib().lite3r_linear_mx_workspace(rows, d_in, d_out, C.byref(a)), "lite3r_linear_mx_workspace")
     return a.value
+
+
+def lite3r_linear_mx_parts(rows: int, d_in: int, d_out: int, sms: int):
+    """(parts of the rows, bytes of the workspace in use) of lite3r_linear_mx_wgrad on a device with this many SMs."""
+    parts, size = C.c_int(), C.c_size_t()
+    _check(lib().lite3r_linear_mx_parts(rows, d_in, d_out, sms, C.byref(parts), C.byref(size)), "lite3r_linear_mx_parts")
+    return parts.value, size.value
 
 
 def lite3r_linear_mx_dgrad(dy: torch.Tensor, w: MxTensor, dx: torch.Tensor, device_status=None, stream=None) -> None:

@@ -772,6 +772,14 @@ lite3r_status lite3r_linear_mx_workspace(int rows, int d_in, int d_out, size_t* 
   return LITE3R_OK;
 }
 
+lite3r_status lite3r_linear_mx_parts(int rows, int d_in, int d_out, int sms, int* parts, size_t* bytes) {
+  const lite3r_status st = check_mx(LITE3R_MXFP8, rows, d_in);
+  if (st != LITE3R_OK) return st;
+  if (parts == nullptr || bytes == nullptr || d_out <= 0 || d_out > 0x7FFFFFFF - 256 || sms <= 0) return LITE3R_ERR_INVALID_ARG;
+  linear_mx_parts(rows, d_in, d_out, sms, parts, bytes);
+  return LITE3R_OK;
+}
+
 static lite3r_status check_mx_back(const void* dy, long long dy_stride, const unsigned char* codes, const unsigned char* scales,
                                    lite3r_mx_format format, int rows, int d_in, int d_out, const int* device_status) {
   lite3r_status st = check_mx(format, rows, d_in);

@@ -270,6 +270,7 @@ lite3r_status launch_linear_mxf4(const uint8_t* x_codes, const uint8_t* x_scales
                                  const float* bias, int rows, int d_in, int d_out, void* y, int y_dtype, long long y_stride,
                                  int* device_status, cudaStream_t stream);
 size_t linear_mx_workspace_bytes(int rows, int d_in, int d_out);
+void linear_mx_parts(int rows, int d_in, int d_out, int sms, int* parts, size_t* bytes);  // see the debug header
 lite3r_status launch_mx_dgrad(const void* dy, long long dy_stride, const uint8_t* w_codes, const uint8_t* w_scales, int format,
                               int rows, int d_in, int d_out, void* dx, int dx_dtype, long long dx_stride, int* device_status,
                               cudaStream_t stream);

@@ -529,7 +529,6 @@ __global__ void __launch_bounds__(256) add_parts_kernel(const Sums dw, int dw_bl
 }
 
 constexpr int kBiasCols = 4;
-constexpr int kMostPairs = 128;  // of any device, for the size of the workspace
 
 // How the tiles are cut.  Columns: all of 256, or the last 256 in two halves, which run last and fill the gaps that whole tiles
 // leave, or halves throughout (few tiles).  A step of a half tile takes three quarters of a whole one's time (0.34 and 0.45 us:
@@ -581,6 +580,29 @@ int wgrad_parts(int rows, int d_in, int d_out, int pairs) {
   return best;
 }
 
+// Numbers of pairs (of devices with 132 to 160 SMs) for whose rule the workspace has room.
+constexpr int kSizedPairs[] = {66, 70, 72, 74, 76, 80};
+
+int most_parts(int rows, int d_in, int d_out) {
+  int parts = 1;
+  for (int pairs : kSizedPairs) parts = std::max(parts, wgrad_parts(rows, d_in, d_out, pairs));
+  return parts;
+}
+
+// The rule's parts, on any other device at most those that the workspace has room for.
+int parts_of_device(int rows, int d_in, int d_out, int pairs) {
+  const int parts = wgrad_parts(rows, d_in, d_out, pairs);
+  for (int sized : kSizedPairs)
+    if (sized == pairs) return parts;
+  return std::min(parts, most_parts(rows, d_in, d_out));
+}
+
+size_t parts_bytes(int parts, int d_in, int d_out) {
+  return ((parts > 1 ? static_cast<size_t>(parts) * d_in * d_out : 0) + static_cast<size_t>(parts) * kGroups * kBiasCols * 4 * d_out) * sizeof(float);
+}
+
+int pairs_of(int sms) { return std::max(1, sms / 2); }
+
 template <int kFormat, bool kWgrad>
 lite3r_status launch_back(const void* dy, long long dy_stride, const uint8_t* codes, const uint8_t* scales, int rows, int d_in,
                           int d_out, const CUtensorMap& map_out, int out_dtype, int parts, float* bias_parts, int* status, int pairs,
@@ -622,17 +644,19 @@ lite3r_status launch_back(const void* dy, long long dy_stride, const uint8_t* co
 lite3r_status pairs_of_device(int* pairs) {
   int sms = 0;
   const lite3r_status st = sm_count(&sms);
-  *pairs = std::max(1, std::min(sms / 2, kMostPairs));
+  *pairs = pairs_of(sms);
   return st;
 }
 
 }  // namespace
 
-// Room for as many parts as any device's rule may choose.
 size_t linear_mx_workspace_bytes(int rows, int d_in, int d_out) {
-  size_t parts = 1;
-  for (int pairs : {66, 70, 72, 74, 76, 80}) parts = std::max<size_t>(parts, wgrad_parts(rows, d_in, d_out, pairs));
-  return ((parts > 1 ? parts * d_in * d_out : 0) + parts * kGroups * kBiasCols * 4 * d_out) * sizeof(float) + 256;
+  return parts_bytes(most_parts(rows, d_in, d_out), d_in, d_out) + 256;
+}
+
+void linear_mx_parts(int rows, int d_in, int d_out, int sms, int* parts, size_t* bytes) {
+  *parts = parts_of_device(rows, d_in, d_out, pairs_of(sms));
+  *bytes = parts_bytes(*parts, d_in, d_out);
 }
 
 lite3r_status launch_mx_dgrad(const void* dy, long long dy_stride, const uint8_t* w_codes, const uint8_t* w_scales, int format,
@@ -659,10 +683,9 @@ lite3r_status launch_mx_wgrad(const void* dy, long long dy_stride, const uint8_t
   int pairs = 0;
   lite3r_status st = pairs_of_device(&pairs);
   if (st != LITE3R_OK) return st;
-  const int parts = wgrad_parts(rows, d_in, d_out, pairs);
+  const int parts = parts_of_device(rows, d_in, d_out, pairs);
   const size_t values = static_cast<size_t>(d_in) * d_out;
-  if (((parts > 1 ? parts * values : 0) + static_cast<size_t>(parts) * kGroups * kBiasCols * 4 * d_out) * sizeof(float) > workspace_bytes)
-    return LITE3R_ERR_WORKSPACE;
+  if (parts_bytes(parts, d_in, d_out) > workspace_bytes) return LITE3R_ERR_WORKSPACE;
   float* const products = parts > 1 ? workspace : dw;
   float* const bias_parts = workspace + (parts > 1 ? parts * values : 0);
   CUtensorMap map;
