@@ -216,9 +216,8 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
     uint32_t parity = 1;  // of the stage's use before, from the second round on
     for (int unit = first_unit; ok && unit < p.units; unit += unit_step) {
       const UnitAt u = unit_at(unit);
-      const int n = u.n0 + rank * (u.half ? 64 : 128);  // this CTA's columns
-      const bool scales = n / 128 < p.scale_tiles;      // (none where they are all past the end)
-      const uint32_t bytes = (u.half ? 1 : 2) * kTileR * L::kBoxBytes + (scales ? kScaleTile : 0);
+      const int n = u.n0 + rank * (u.half ? 64 : 128);  // this CTA's columns; n / 128 is a scale tile (cut_tiles makes no tile past them)
+      const uint32_t bytes = (u.half ? 1 : 2) * kTileR * L::kBoxBytes + kScaleTile;
       const int x = kFormat == LITE3R_MXFP8 ? n : n / 2;
       for (int k = u.first; ok && k < u.last; ++k, ++kc) {
         if (kc >= kRaw) ok = mbar_wait_clearing(&bars->raw_empty[st], parity, abort_flag, p.status, 811);
@@ -229,9 +228,8 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
           mbar_arrive_expect_tx(&bars->raw_full[st], bytes);
           tma_load_2d(dst, &map_codes, &bars->raw_full[st], x, k * kTileR);
           if (!u.half) tma_load_2d(dst + kTileR * L::kBoxBytes, &map_codes, &bars->raw_full[st], x + L::kBoxBytes, k * kTileR);
-          if (scales)
-            bulk_load(dst + L::kOffScales, p.scales + (static_cast<size_t>(k / 2) * p.scale_tiles + n / 128) * kScaleTile, kScaleTile,
-                      &bars->raw_full[st]);
+          bulk_load(dst + L::kOffScales, p.scales + (static_cast<size_t>(k / 2) * p.scale_tiles + n / 128) * kScaleTile, kScaleTile,
+                    &bars->raw_full[st]);
         }
         if (++st == kRaw) {
           st = 0;
