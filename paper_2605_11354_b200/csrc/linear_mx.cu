@@ -259,7 +259,7 @@ linear_mxf4_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_const
       float* const bia = reinterpret_cast<float*>(smem + L::kOffBias) + ab * kN + hh * 64;
       if (tid < 64) bia[tid] = (p.bias != nullptr && col + tid < p.d_out) ? __ldg(p.bias + col + tid) : 0.f;
       named_barrier_sync(1 + hh, 128);
-      ok = mbar_wait_clearing(&bars->acc_full[ab], (it >> 1) & 1, abort_flag, p.status, 803);
+      ok = mbar_wait_clearing(&bars->acc_full[ab], (it >> 1) & 1, abort_flag, p.status, 803, 0, sum_limit_ns(stages_k));
       tc_fence_after();
       ok = __all_sync(0xFFFFFFFFu, ok);
       if (!ok) break;

@@ -412,7 +412,7 @@ mx_back_kernel(const __grid_constant__ CUtensorMap map_dy, const __grid_constant
         const int ab = it & 1;
         const bool add = k0 > u.first;  // to the sum before, which this warp has stored
         const uint32_t acc_addr = tmem + ((static_cast<uint32_t>(quarter) * 32u) << 16) + ab * kTileN;
-        ok = mbar_wait_clearing(&bars->acc_full[ab], (it >> 1) & 1, abort_flag, p.status, 813);
+        ok = mbar_wait_clearing(&bars->acc_full[ab], (it >> 1) & 1, abort_flag, p.status, 813, 0, sum_limit_ns(p.steps_per_sum));
         tc_fence_after();
         ok = __all_sync(0xFFFFFFFFu, ok);
         if (!ok) break;

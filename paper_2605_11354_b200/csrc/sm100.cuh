@@ -92,6 +92,8 @@ __device__ __forceinline__ uint64_t global_timer_ns() {
 // backoff_ns > 0 makes the thread sleep between polls: for single-thread roles whose waits are long, so that their
 // polling does not take issue slots from the working warps.
 constexpr uint64_t kWaitLimitNs = 1000000000ull;  // 1 s
+// The limit of a wait for a whole sum of `steps` steps of a contraction: 2 us a step (they take 0.3 to 0.5) on top.
+__device__ __forceinline__ uint64_t sum_limit_ns(int steps) { return kWaitLimitNs + 2000ull * static_cast<uint64_t>(steps); }
 // What a waiting thread looks at every few polls: returns the time at which the wait began (since = 0: now), or 0 when
 // the wait is over without success.
 __device__ __forceinline__ uint64_t wait_check(uint64_t since, volatile int* abort_flag, int* status, int code, uint64_t limit_ns) {
@@ -144,8 +146,8 @@ __device__ __forceinline__ bool mbar_wait_far(uint64_t* bar, uint32_t parity, vo
 // The wait of a kernel that clears the status word itself (its first CTA does, long before any wait can expire): the word
 // is written when a wait expires but not looked at, since it may still hold what an earlier call left.
 __device__ __forceinline__ bool mbar_wait_clearing(uint64_t* bar, uint32_t parity, volatile int* abort_flag, int* status,
-                                                   int code, uint32_t backoff_ns = 0) {
-  if (mbar_wait(bar, parity, abort_flag, nullptr, code, backoff_ns)) return true;
+                                                   int code, uint32_t backoff_ns = 0, uint64_t limit_ns = kWaitLimitNs) {
+  if (mbar_wait(bar, parity, abort_flag, nullptr, code, backoff_ns, limit_ns)) return true;
   if (status != nullptr) atomicCAS(status, 0, code);
   return false;
 }

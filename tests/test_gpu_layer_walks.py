@@ -235,3 +235,50 @@ def test_backward_pairs_give_the_same_bits_each_time(rows, d_in, d_out, w_fmt, x
                 differing[i] += torch.stack([(a != b).sum() for a, b in zip(again[i], first)])
     torch.cuda.synchronize()
     assert not any(d.any() for d in differing), differing
+
+
+# ------------------------------------------------------------------------------------------------------ very long contractions
+def places(n, seed):
+    """Some hundred places below n, the first and last among them."""
+    p = np.random.default_rng(seed).integers(0, n, 300)
+    return torch.from_numpy(np.unique(np.concatenate([p, [0, 1, n // 2, n - 1]]))).cuda()
+
+
+def test_a_product_that_takes_seconds():
+    """One row by one column of 3 x 2^29 elements: one sum of 6 million steps, longer than a wait on a barrier may take otherwise.  Nearly
+    all elements are zero, so the sum of the others, multiples of 1/4, is exact."""
+    n = 3 << 29
+    at = places(n // 2, 1)  # bytes of two codes
+    g = torch.Generator(device="cuda").manual_seed(2)
+    values, operands = [], []
+    for _ in range(2):
+        codes = torch.zeros((1, n // 2), dtype=torch.uint8, device="cuda")
+        byte = torch.randint(0, 256, (len(at),), generator=g, device="cuda").to(torch.uint8)
+        codes[0, at] = byte
+        scales = torch.zeros((1, n // 128, 32, 4, 4), dtype=torch.uint8, device="cuda")
+        scales[:, :, 0, 0] = 127
+        operands.append(lt.MxTensor(codes, scales, 1, n))
+        table = torch.tensor([0, 0.5, 1, 1.5, 2, 3, 4, 6, 0, -0.5, -1, -1.5, -2, -3, -4, -6], dtype=torch.float64, device="cuda")
+        values.append(torch.stack([table[(byte & 15).long()], table[(byte >> 4).long()]]))
+    y, status = torch.full((1, 8), 9.0, device="cuda")[:, :1], torch.ones(1, dtype=torch.int32, device="cuda")
+    lt.lite3r_linear_mxfp4(operands[0], operands[1], None, y, status)
+    assert int(status.item()) == 0
+    assert float(y.item()) == float((values[0] * values[1]).sum())
+
+
+def test_an_input_gradient_that_takes_seconds():
+    """The same for a layer of 3 x 2^27 outputs and a 16-bit result (fp32 results are sums of 2048 steps of the contraction)."""
+    n, d_in = 3 << 27, 32
+    at = places(n, 3)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    codes = torch.zeros((n, d_in // 2), dtype=torch.uint8, device="cuda")
+    codes[at] = 0x24  # 1 in the odd columns and 2 in the even ones
+    scales = torch.full((n // 128, 1, 32, 4, 4), 127, dtype=torch.uint8, device="cuda")
+    dy = torch.zeros((1, n), dtype=torch.bfloat16, device="cuda")
+    dy[0, at] = torch.randint(-4, 5, (len(at),), generator=g, device="cuda").bfloat16()
+    dx, status = torch.full((1, d_in), 9.0, dtype=torch.float16, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    lt.lite3r_linear_mx_dgrad(dy, lt.MxTensor(codes, scales, n, d_in), dx, status)
+    assert int(status.item()) == 0
+    total = float(dy[0, at].double().sum())
+    assert abs(total) < 1024
+    assert dx[0, 0::2].tolist() == [2 * total] * 16 and dx[0, 1::2].tolist() == [total] * 16  # whole numbers below 2048
