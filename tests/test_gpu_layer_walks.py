@@ -282,3 +282,70 @@ def test_an_input_gradient_that_takes_seconds():
     total = float(dy[0, at].double().sum())
     assert abs(total) < 1024
     assert dx[0, 0::2].tolist() == [2 * total] * 16 and dx[0, 1::2].tolist() == [total] * 16  # whole numbers below 2048
+
+
+@pytest.mark.parametrize("rows,d_in,d_out", [(130, 65536, 72), (2000, 32768, 2504)])
+def test_a_long_running_sum_of_the_4_bit_layer(rows, d_in, d_out):
+    """All terms positive, block scales spread over 2^6: the running sum is cut off at fp32 after every product of 64 elements, by
+    less than 2 u of what it is then, which is at most the result: 2 u d_in / 64 in all, and nothing is added after."""
+    def operand(seed, n):
+        g = torch.Generator(device="cuda").manual_seed(seed)
+        x = (0.5 + torch.rand((n, d_in // 32, 32), generator=g, device="cuda")) * torch.exp2(torch.randint(0, 7, (n, d_in // 32, 1), generator=g,
+                                                                                                         device="cuda").float())
+        t = lt.lite3r_quantize_mx(x.view(n, d_in), "mxfp4")
+        return t, lt.lite3r_dequantize_mx(t, torch.empty((n, d_in), device="cuda")).double()
+
+    (x, xv), (w, wv) = operand(1, rows), operand(2, d_out)
+    y = torch.empty((rows, d_out), device="cuda")
+    lt.lite3r_linear_mxfp4(x, w, None, y)
+    off = (y.double() / (xv @ wv.t()) - 1)
+    assert off.abs().max().item() <= 2 * U * (d_in / 64 + 1), (off.min().item() / U, off.max().item() / U)
+    print(f"off by {off.mean().item() / U / (d_in / 64):.3f} u a product, {off.min().item() / U:.1f} to {off.max().item() / U:.1f} u")
+
+
+# ------------------------------------------------------------------------------------------------------ more than 2^31 elements
+def test_matrices_of_more_elements_than_an_index_of_32_bits_has():
+    rows, cols = 70001, 32768
+    assert rows * cols > 2 ** 31
+    g = torch.Generator(device="cuda").manual_seed(7)
+    x = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda")
+    for r in range(0, rows, 10000):
+        x[r:r + 10000] = torch.randn((min(10000, rows - r), cols), generator=g, device="cuda", dtype=torch.bfloat16)
+    # the last tile of 128 rows (and what is left of it) as a matrix of its own
+    tail = rows // 128 * 128 - 128
+    for fmt in ("mxfp4", "mxfp8"):
+        t, part = lt.lite3r_quantize_mx(x, fmt), lt.lite3r_quantize_mx(x[tail:], fmt)
+        assert torch.equal(t.codes[tail:], part.codes) and torch.equal(t.scales[tail // 128:], part.scales)
+        back = lt.lite3r_dequantize_mx(t, torch.empty_like(x))
+        assert torch.equal(back[tail:], lt.lite3r_dequantize_mx(part, torch.empty_like(x[tail:])))
+        assert torch.equal(back[:300], lt.lite3r_dequantize_mx(lt.lite3r_quantize_mx(x[:300], fmt), torch.empty_like(x[:300])))
+        del t, back
+    del x
+    # a result, an input gradient and a weight gradient of that size
+    few = 64
+    a, w = lt.lite3r_quantize_mx(torch.randn((rows, few), generator=g, device="cuda")), lt.lite3r_quantize_mx(torch.randn((cols, few), generator=g, device="cuda"))
+    y = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda")
+    lt.lite3r_linear_mxfp4(a, w, None, y)
+    av, wv = (lt.lite3r_dequantize_mx(t, torch.empty((t.rows, few), device="cuda")).double() for t in (a, w))
+    pick = torch.cat([torch.arange(200, device="cuda"), torch.arange(rows - 200, rows, device="cuda")])
+    size = av[pick].abs() @ wv.abs().t()
+    all_within(y[pick], av[pick] @ wv.t(), 2 * U * (few / 64 + 2) * size, y.dtype, "y")
+    del y
+    dy = torch.randn((rows, few), generator=g, device="cuda").bfloat16()
+    wide = lt.lite3r_quantize_mx(torch.randn((few, cols), generator=g, device="cuda"), "mxfp4")
+    dx = torch.empty((rows, cols), dtype=torch.bfloat16, device="cuda")
+    lt.lite3r_linear_mx_dgrad(dy, wide, dx)
+    value = lt.lite3r_dequantize_mx(wide, torch.empty((few, cols), device="cuda")).double()
+    d = dy[pick].double()
+    all_within(dx[pick], d @ value, 2 * U * (few / 16 + 8) * (d.abs() @ value.abs()), dx.dtype, "dx")
+    del dx
+    outputs = rows // 8 * 8
+    kept = lt.lite3r_quantize_mx(torch.randn((few, cols), generator=g, device="cuda"), "mxfp8")
+    dy = torch.randn((few, outputs), generator=g, device="cuda").bfloat16()
+    dw, db = torch.empty((outputs, cols), device="cuda"), torch.empty(outputs, device="cuda")
+    lt.lite3r_linear_mx_wgrad(dy, kept, dw, db, base.workspace(lt.lite3r_linear_mx_workspace(few, cols, outputs)))
+    value = lt.lite3r_dequantize_mx(kept, torch.empty((few, cols), device="cuda")).double()
+    pick = torch.cat([torch.arange(200, device="cuda"), torch.arange(outputs - 200, outputs, device="cuda")])
+    d = dy[:, pick].double().t()
+    all_within(dw[pick], d @ value, 2 * U * (few / 16 + 8) * (d.abs() @ value.abs()), dw.dtype, "dw")
+    all_within(db, dy.double().sum(0), (few + 8) * U * dy.double().abs().sum(0), db.dtype, "db")
