@@ -484,8 +484,9 @@ RopeParams params_of(const lite3r_rope& how) {
   return p;
 }
 
-// Parts of a token's heads: as many heads to a part as leave every SM `ctas` CTAs, so that a token's coefficients serve many
-// heads; one head at the fewest tokens.
+// Parts of a token's heads: as many heads to a part as leave every SM its `ctas` resident CTAs, so that a token's coefficients
+// serve many heads; one head at the fewest tokens.  (Counted for a CTA more than reside, the forward of two frames took 11.9 us
+// instead of 7.5, of eight 17.4 instead of 16.8.)
 void set_chunks(RopeTensor& t, long long tokens_all, int dim, int most, int sms, int ctas) {
   if (t.heads == 0) return;
   const long long groups = static_cast<long long>(sms) * ctas * (kRopeThreads / (dim / 16));
@@ -528,7 +529,7 @@ lite3r_status launch_rope(const lite3r_tensor* q, const lite3r_tensor* k, const 
   RopeParams p = params_of(how);
   p.t[0] = tensor_of(q, nullptr, q_out, how.q_weight, how.q_bias, how.q_heads);
   p.t[1] = tensor_of(k, nullptr, k_out, how.k_weight, how.k_bias, how.k_heads);
-  for (RopeTensor& x : p.t) set_chunks(x, p.tokens_all, how.head_dim, 16, sms, 5);
+  for (RopeTensor& x : p.t) set_chunks(x, p.tokens_all, how.head_dim, 16, sms, kRopeCtas);
   const int groups = kRopeThreads / (how.head_dim / 16);
   const long long blocks = (p.tokens_all + groups - 1) / groups;
   const int parts = p.t[0].chunks + p.t[1].chunks;

@@ -47,8 +47,8 @@ def all_within(got, ref, tol, dtype, what):
 
 # ------------------------------------------------------------------------------------------------------ walks over heads
 # B, H, K, N, D, axes, norm, dtype.  With 148 SMs the forward gives a group of lanes
-#   3 of 10 heads and 1 of 5;   12 of 24 and 4 of 7;   16 of 16;   4 of 7 and 2 of 3;   3 of 5 and 12 of 24
-# and of the last two 3 and 1, 5;  the gradient 4 and 2;  4 and 4;  4;  4 and 3;  3 and 4;  4 and 3;  3, in two to nine steps of the grid.
+#   4 of 10 heads and 2 of 5;   12 of 24 and all 7;   all 16;   all 7 and all 3;   all 5 and 12 of 24;   4 of 10 and 2 of 5;   all 5
+# and the gradient 4 and 2;  4 and 4;  4;  4 and 3;  3 and 4;  4 and 3;  3, in two to nine steps of the grid.
 WALKS = [(3, 10, 5, 3001, 64, 1, "rms", "bf16"), (2, 24, 7, 10000, 64, 2, "layer", "bf16"), (1, 16, 16, 32003, 64, 2, "layer", "f16"),
          (1, 7, 3, 10007, 128, 1, "rms", "f16"), (4, 5, 24, 10001, 32, 2, "layer", "f32"), (3, 10, 5, 3001, 64, 0, "layer", "f32"),
          (1, 5, 5, 9001, 256, 2, "none", "f32")]
