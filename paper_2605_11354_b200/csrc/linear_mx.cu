@@ -1,7 +1,9 @@
 // The linear layer on microscaled 4-bit operands: y = Q(x) Q(W)^T + b with block-scaled tcgen05 products (e2m1 x e2m1, one
 // scale per 32 elements of K, fp32 accumulation in TMEM).
-// A product of two e2m1 values is a multiple of 1/4 below 2^6 and the scales are powers of two, so the fp32 accumulation is
-// exact but for scales that lie many powers of two apart.
+// A product of two e2m1 values is a multiple of 1/4 of at most 36 (8 bits) and the scales are powers of two, so a sum of K of them
+// in fp32 is exact while the scales' spread along it (of both operands together) is below 2^(24 - 8 - log2 K): 2^4 for 4096
+// elements.  Beyond that the running sum is cut off, not rounded: low by 0.07 to 0.11 x 2^-24 of the result for every product of
+// 64 elements where all terms are positive and the blocks' scales lie within 2^6 (4096 elements: 4e-7).  One sum over all of d_in.
 // Persistent CTAs over tiles of 128 rows x 64 or 128 columns, or pairs of CTAs (cta_group::2, half of A's and of B's rows
 // each) over tiles of 256 x 256.  Warp 0 loads A and B as bytes (rows of 128 = 256 elements of K, 128B swizzle), warp 2 the scale
 // tiles of both as they lie in memory, warp 1 copies the scales to tensor memory and issues the products into one of two
@@ -9,9 +11,10 @@
 // shared memory.  The products of the next tile run under the epilogue of this one.
 // Tensor memory: two accumulators of 256 columns leave no room for the scales, so they share 32 columns: the warpgroup that
 // has these reads them first, and the next tile's products wait for that (a few hundred cycles) and not for the epilogue.
-// 43968 x 4096 x 1024 in 69 us, 5.3 PFLOP/s, the tensor pipe busy for 70 % of it (by single CTAs on 128 x 128: 162 us).  A stage of
-// 256 elements of K takes 720 cycles: 560 of products and 100 of scale copies, which run in order with them, and at the end of a
-// tile the wait for the shared columns.  10992 x 1024 x 4096 in 26 us.
+// 43968 x 4096 x 1024 in 69 to 76 us (the first at 1.97 GHz: 5.3 PFLOP/s), the tensor pipe busy for 70 % of it, and 88 us in a run of
+// a second, where the power limit leaves 1.43 GHz (by single CTAs on 128 x 128: 162 us).  A stage of 256 elements of K takes 720
+// cycles: 560 of products and 100 of scale copies, which run in order with them, and at the end of a tile the wait for the shared
+// columns.  10992 x 1024 x 4096 in 26 to 28 us.
 // Every mbarrier wait is bounded; on expiry the CTA sets *device_status and its roles leave their loops.
 #include <algorithm>
 

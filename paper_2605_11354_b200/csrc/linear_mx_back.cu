@@ -11,10 +11,14 @@
 // the pair's first CTA issues the products into one of two accumulators, four warps are the epilogue.
 // The sixteen warps work in four groups, each on every fourth step: a step's chain of load, arithmetic, store and proxy fence
 // takes longer than its products (1900 cycles of a step with all warps on the same one, 512 of products), four chains side by
-// side do not.  Each CTA converts half of B for the pair.  10992 x 1024 x 4096 (92 GFLOP each): dgrad 75 us, wgrad 79, or 85 with
-// db, the tensor pipe busy for 62 to 64 % (76 us with the conversion left out: shared memory carries the products' operands, dy,
-// the codes and what is made of them).  For db the groups also add up the columns of dy while its tile lies
-// in shared memory, the first four column tiles by turns.
+// side do not.  Each CTA converts half of B for the pair.  10992 x 1024 x 4096 (92 GFLOP each): dgrad 75 us, wgrad 81, or 90 with
+// db, the tensor pipe busy for 62 to 65 %; in a run of a second, at the 1.5 GHz that the power limit leaves, 88, 95 and 102.
+// (76 us with the conversion left out: shared memory carries the products' operands, dy, the codes and what is made of them.  A
+// group also holds one of the five stages of operands through its arithmetic; and wgrad's 64 tiles leave 10 of 74 pairs idle.)
+// For db the groups also add up the columns of dy while its tile lies in shared memory, the first four column tiles by turns.
+//
+// The second CTA's warps tell the first one that their half is there by 16 bytes of it, copied to a place there that nothing
+// reads, which the first one's barrier counts.
 //
 // The tensor cores' running sum is cut off, not rounded, at fp32: it drifts towards zero by about 4e-9 of the result per
 // product of 16 steps (10992 rows in one sum: dW off by 2.6e-6).  Results in fp32 are therefore summed over 2048 steps at a time

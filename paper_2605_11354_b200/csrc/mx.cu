@@ -8,8 +8,9 @@
 // The scales lie in tiles of 128 rows x 4 blocks (512 bytes), row r at (r % 32) * 16 + (r / 32) * 4: the layout from which the
 // tensor cores take them, so a product copies a tile as it is.  A CTA makes one such tile, 128 rows x 128 values: its 512
 // scale bytes meet in shared memory and leave in one piece, and each of its threads has eight independent loads under way.
-// Bound by HBM: 43968 x 4096 bf16 values to 4 bits in 69 us (455 MB, 6.6 TB/s), to 8 bits in 80 (546 MB), back in 84.  With scalar
-// maxima, products and conversions it was bound by its 100 instructions per 256 values (now 59): 99 us.
+// Bound by HBM: 43968 x 4096 bf16 values to 4 bits in 67 us (456 MB, 6.8 TB/s), to 8 bits in 81 (546 MB), back in 72 and 86, 6.3 TB/s
+// (in a run of a second at the power limit 74, 86, 75 and 89).  With scalar maxima, products and conversions it was bound by its
+// 100 instructions per 256 values (now 59): 99 us.
 #include <algorithm>
 
 #include <cuda_fp4.h>

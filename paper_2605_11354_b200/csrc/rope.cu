@@ -8,8 +8,10 @@
 // 64 values take two shuffles.  A group of lanes stays with one token and walks its heads
 // while the next ones' loads are under way; sine, cosine, weight and bias meet in six coefficients per pair, made once per
 // token.  Arithmetic on packed pairs of fp32.
-// 32 frames of 1374 tokens, 16 heads of 64 bf16 queries and keys: 67 us, 5.4 TB/s (172 us with four pairs to a lane and scalar
-// arithmetic, 159 instructions per 256 values); a hundred frames 188 us, 6.0 TB/s; the gradient of 32 frames 116 us, 4.7 TB/s.
+// 32 frames of 1374 tokens, 16 heads of 64 bf16 queries and keys: 66 us, 5.5 TB/s (172 us with four pairs to a lane and scalar
+// arithmetic, 159 instructions per 256 values); a hundred frames 184 us, 6.1 TB/s; the gradient of 32 frames 115 us, 4.7 TB/s.
+// In fp32: 32 frames 136 us, 5.3 TB/s; the gradient of 16 frames 106 us, 5.1 TB/s.  (Single calls at full clocks; in a run of a
+// second at the power limit 2 to 5 % longer.)
 // Angles: position * base^(-2i/S) / 2 pi in 64-bit fixed point (an fp32 product of a position of a million is off by a tenth of
 // a radian), whose overflow leaves the fraction of a turn; that in fp32.  Sums and norms are fp32; results are rounded once.
 #include <algorithm>
@@ -302,8 +304,10 @@ __global__ void __launch_bounds__(kRopeThreads, kRopeCtas) rope_kernel(const __g
 // Gradient of one tensor (blockIdx.y: queries or keys).  Groups of lanes walk tokens (and parts of their heads) in steps of
 // the grid and keep dw and db of their sixteen elements in registers; a CTA adds its groups in order and leaves one partial.
 // The weight lies in shared memory: registers hold the sums, the angles' sines and cosines and the next row on its way.
-// (Rows through a ring in shared memory, three ahead and across tokens, took as long: not the loads but the 300 instructions
-// of 512 values and their latency bound it.)
+// Two bounds lie close together.  Instructions: four warps to a scheduler take 60 % of its issue slots, and of the time in which a
+// warp is stalled 32 % goes to results of fixed latency, 20 % to busy pipes, 19 % to shuffles and shared memory, 26 % to loads.
+// Loads: with the arithmetic left out one row ahead still takes 110 us of 115 (and a plain addition over the same three
+// streams 88).  Rows through a ring in shared memory, three ahead and across tokens, mend the second at the cost of the first: 125.
 template <typename T, int kDim>
 __global__ void __launch_bounds__(kRopeThreads, back_ctas(sizeof(T))) rope_back_kernel(const __grid_constant__ RopeParams p) {
   constexpr int kLanes = kDim / 16;
