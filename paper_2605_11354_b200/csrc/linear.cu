@@ -330,7 +330,10 @@ linear_fp8_kernel(const __grid_constant__ CUtensorMap map_x, const __grid_consta
       for (int tile_id = first_tile; ok && tile_id < p.tiles; tile_id += tile_step, ++it) {
         const int ab = it & 1;
         // the accumulator was last used two tiles ago: wait until the epilogue warps have read it out
-        if (it >= 2) ok = mbar_wait_clearing(&bars->acc_empty[ab], ((it - 2) >> 1) & 1, abort_flag, p.status, 604);
+        if (it >= 2) {
+          if constexpr (kPair) ok = mbar_wait_cluster_clearing(&bars->acc_empty[ab], ((it - 2) >> 1) & 1, abort_flag, p.status, 604);
+          else ok = mbar_wait_clearing(&bars->acc_empty[ab], ((it - 2) >> 1) & 1, abort_flag, p.status, 604);
+        }
         tc_fence_after();
         for (int k = 0; ok && k < k_steps; ++k, ++kc) {
           const int st = kc % kStages;

@@ -47,3 +47,14 @@ def test_the_workspace_has_room_on_every_device():
 def test_parts_refuse_what_is_no_layer(args):
     with pytest.raises(lt.Lite3rError):
         lt.lite3r_linear_mx_parts(*args)
+
+
+def test_waits_for_another_cta_have_its_scope():
+    """A kernel that sends arrivals to its pair's first CTA waits for them there at cluster scope, too."""
+    for name in sorted(os.listdir(lb.CSRC)):
+        with open(os.path.join(lb.CSRC, name)) as f:
+            text = f.read()
+        if not name.endswith(".cu") or "mbar_arrive_cluster" not in text:
+            continue
+        waits = re.findall(r"(mbar_wait_cluster_clearing(?:<true>)?\(\s*|wait_read\(\s*|mbar_wait_clearing\(\s*)&bars->(acc_empty|shared_read)", text)
+        assert any(how.startswith(("mbar_wait_cluster", "wait_read")) for how, _ in waits), (name, waits)
